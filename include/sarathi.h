@@ -222,6 +222,51 @@ sarathi_status sarathi_hybrid_attention_noalloc(sarathi_handle *handle,
                                                 int32_t num_seqs, int32_t num_tokens, int64_t num_pages,
                                                 float sm_scale, void *out, void *stream);
 
+/* ---- The same path over a cache held in 4 bits ------------------------------------------------------
+ * One pool instead of two, a quarter of the bytes: a page (of page_size = 16 positions) holds a RECORD for each KV head,
+ *
+ *   kv_cache + (page*num_kv_heads + h) * (16.5*head_dim + 64) bytes:
+ *     keys     [head_dim/32 blocks][16 slots][16 bytes]   channels 32 b + 2 j, 2 j + 1 in the low and high half of byte j
+ *     values   [4 quads][16][head_dim/16][2 bytes]        byte i/2 of [quad][n][c]: channel 16 c + n of slot 4 quad + i, even i in the low half
+ *     scales   of the keys [head_dim/32][16 slots] bytes, then of the values [16 slots] floats
+ *
+ * of 4-bit numbers with a sign (the high bit) and the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6.  Rounding is to the nearest one, ties to
+ * the even code, and what is larger becomes 6.  A key's block of 32 channels has a scale 2^e, held as the byte e + 127: the smallest with
+ * max |k| <= 6 * 2^e, e in -100 .. 124.  The values of a position and KV head have one scale m * 2^e with m in 8 .. 15: the smallest with
+ * max |v| <= 6 * m * 2^e, not below 2^-100, not above 2^124.  A block of keys that holds an infinity or NaN has the byte 255 and stands for
+ * NaN; values that hold one have the scale NaN.  What a record stands for is exact in bf16.  Hidden positions (beyond ctx_len, behind
+ * a row's own, in front of its window) influence no result, whatever their slots hold, NaN and infinities included.
+ *
+ * sarathi_quantised_page_bytes: bytes of a page, all KV heads.  kv_cache, k_new, v_new, k_rows and v_rows are 16-byte aligned, else
+ * SARATHI_EINVAL.  Everything else is as for the functions of the same name without _quantised: a handle serves both kinds of
+ * cache, one plan of an append is used by an attention call over the same kind only.  Of a page that is written in part, the
+ * other slots keep what they held. */
+size_t sarathi_quantised_page_bytes(const sarathi_handle *handle);
+sarathi_status sarathi_kv_append_quantised(sarathi_handle *handle, const void *k_new, const void *v_new, void *kv_cache,
+                                           const int32_t *block_table,
+                                           const int32_t *q_start, const int32_t *q_len, const int32_t *ctx_len,
+                                           int32_t num_seqs, int32_t num_tokens, int64_t num_pages,
+                                           void *workspace, void *stream);
+/* The way back: k_rows and v_rows (dev, bf16 [num_tokens, Hkv, head_dim], batch order, written) receive what the cache holds of
+ * positions ctx_len-q_len .. ctx_len-1 of each sequence.  Rows of a page that the block table gives out of range stay as they were.
+ * Needs no workspace; not for stream capture. */
+sarathi_status sarathi_kv_read_quantised(sarathi_handle *handle, const void *kv_cache, const int32_t *block_table,
+                                         const int32_t *q_start, const int32_t *q_len, const int32_t *ctx_len,
+                                         int32_t num_seqs, int32_t num_tokens, int64_t num_pages,
+                                         void *k_rows, void *v_rows, void *stream);
+sarathi_status sarathi_hybrid_attention_quantised(sarathi_handle *handle, const void *q, const void *kv_cache,
+                                                  const int32_t *block_table,
+                                                  const int32_t *q_start, const int32_t *q_len, const int32_t *ctx_len,
+                                                  int32_t num_seqs, int32_t num_tokens, int64_t num_pages,
+                                                  float sm_scale, void *out, void *workspace, void *stream);
+/* For callers under stream capture or without a workspace, with the limits of sarathi_hybrid_attention_noalloc and on the same
+ * scratch array of the GPU. */
+sarathi_status sarathi_hybrid_attention_quantised_noalloc(sarathi_handle *handle, const void *q, const void *kv_cache,
+                                                          const int32_t *block_table,
+                                                          const int32_t *q_start, const int32_t *q_len, const int32_t *ctx_len,
+                                                          int32_t num_seqs, int32_t num_tokens, int64_t num_pages,
+                                                          float sm_scale, void *out, void *stream);
+
 /* Host-only view of the work decomposition sarathi_hybrid_attention would launch for this
  * description (no device work).  For tests and for sizing studies. */
 typedef struct {

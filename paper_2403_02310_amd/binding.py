@@ -70,7 +70,8 @@ EXPORTED = ["sarathi_create", "sarathi_destroy", "sarathi_workspace_bytes", "sar
             "sarathi_set_option", "sarathi_kv_append", "sarathi_hybrid_attention",
             "sarathi_plan_hybrid_attention", "sarathi_build_stall_free_batch", "sarathi_get_kernel_times",
             "sarathi_linear", "sarathi_linear_workspace_bytes", "sarathi_plan_linear", "sarathi_plan_linear_rest",
-            "sarathi_hybrid_attention_noalloc"]
+            "sarathi_hybrid_attention_noalloc", "sarathi_quantised_page_bytes", "sarathi_kv_append_quantised",
+            "sarathi_kv_read_quantised", "sarathi_hybrid_attention_quantised", "sarathi_hybrid_attention_quantised_noalloc"]
 
 if not os.path.exists(LIB_PATH):
     raise ImportError("libsarathi.so is not built: run `python -c 'import __graft_entry__ as g; g.build()'` "
@@ -106,6 +107,17 @@ lib.sarathi_hybrid_attention.argtypes = [_vp, _vp, _vp, _vp, _vp, _i32p, _i32p, 
 lib.sarathi_hybrid_attention_noalloc.restype = ctypes.c_int
 lib.sarathi_hybrid_attention_noalloc.argtypes = [_vp, _vp, _vp, _vp, _vp, _i32p, _i32p, _i32p,
                                                  ctypes.c_int32, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, _vp, _vp]
+_batch = [_vp, _i32p, _i32p, _i32p, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64]  # block table, lengths, counts
+lib.sarathi_quantised_page_bytes.restype = ctypes.c_size_t
+lib.sarathi_quantised_page_bytes.argtypes = [_vp]
+lib.sarathi_kv_append_quantised.restype = ctypes.c_int
+lib.sarathi_kv_append_quantised.argtypes = [_vp, _vp, _vp, _vp] + _batch + [_vp, _vp]
+lib.sarathi_kv_read_quantised.restype = ctypes.c_int
+lib.sarathi_kv_read_quantised.argtypes = [_vp, _vp] + _batch + [_vp, _vp, _vp]
+lib.sarathi_hybrid_attention_quantised.restype = ctypes.c_int
+lib.sarathi_hybrid_attention_quantised.argtypes = [_vp, _vp, _vp] + _batch + [ctypes.c_float, _vp, _vp, _vp]
+lib.sarathi_hybrid_attention_quantised_noalloc.restype = ctypes.c_int
+lib.sarathi_hybrid_attention_quantised_noalloc.argtypes = [_vp, _vp, _vp] + _batch + [ctypes.c_float, _vp, _vp]
 lib.sarathi_plan_hybrid_attention.restype = ctypes.c_int
 lib.sarathi_plan_hybrid_attention.argtypes = [_vp, _i32p, _i32p, _i32p, ctypes.c_int32, ctypes.c_int32,
                                               ctypes.POINTER(PlanInfo), ctypes.POINTER(WorkItem), ctypes.c_int32]
@@ -194,6 +206,8 @@ _as_pointer = _taken_as(_vp)
 _marshal.conversions(_taken_as(ctypes.c_int32), _taken_as(ctypes.c_int64), _address)
 _marshal.setup(*(ctypes.cast(f, _vp).value for f in (lib.sarathi_kv_append, lib.sarathi_hybrid_attention, lib.sarathi_hybrid_attention_noalloc)),
                np.ndarray, _i32, _current_stream, _check_block_table)
+_marshal.setup_quantised(*(ctypes.cast(f, _vp).value for f in (lib.sarathi_kv_append_quantised, lib.sarathi_kv_read_quantised,
+                                                                lib.sarathi_hybrid_attention_quantised, lib.sarathi_hybrid_attention_quantised_noalloc)))
 
 
 class Handle:
@@ -288,6 +302,58 @@ class Handle:
         """``sarathi_hybrid_attention_noalloc``: no workspace, the library's built-in scratch."""
         self._check(_marshal.attention(self._address(), self.config.max_blocks_per_seq, q, k_cache, v_cache, block_table,
                                        q_start, q_len, ctx_len, num_pages, num_tokens, float(sm_scale), out, stream))
+        return out
+
+
+    # ---- the same over the 4-bit cache -----------------------------------
+    def quantised_cache_shape(self, num_pages: int) -> tuple:
+        """Shape of the uint8 pool of the 4-bit cache: a record for each page and KV head."""
+        heads = self.config.num_kv_heads
+        return num_pages, heads, int(lib.sarathi_quantised_page_bytes(self._h)) // heads
+
+    def _check_quantised(self, kv_cache, rows=(), num_tokens: Optional[int] = None, q_len=()) -> None:
+        """The C ABI takes bare pointers; a pool or rows of another shape or type would be walked with the handle's."""
+        shape = getattr(kv_cache, "shape", None)
+        if shape is not None and (len(shape) != 3 or kv_cache.element_size() != 1 or tuple(shape) != self.quantised_cache_shape(int(shape[0]))):
+            raise ValueError("kv_cache must be bytes of shape %s, got %s of %s"
+                             % (("pages",) + self.quantised_cache_shape(0)[1:], tuple(shape), getattr(kv_cache, "dtype", None)))
+        for r in rows:
+            shape = getattr(r, "shape", None)
+            if shape is None:
+                continue
+            want = int(np.sum(q_len)) if num_tokens is None else num_tokens
+            if len(shape) != 3 or tuple(shape[1:]) != (self.config.num_kv_heads, self.config.head_dim) or int(shape[0]) < want or r.element_size() != 2:
+                raise ValueError("rows must be bf16 [>= %d, %d, %d], got %s" % (want, self.config.num_kv_heads, self.config.head_dim, tuple(shape)))
+
+    def kv_append_quantised(self, k_new, v_new, kv_cache, block_table, q_start, q_len, ctx_len, num_pages: Optional[int] = None,
+                            num_tokens: Optional[int] = None, workspace=None, stream=None):
+        """``sarathi_kv_append_quantised``: the new rows in 4 bits into ``kv_cache``, uint8 of ``quantised_cache_shape``."""
+        self._check_quantised(kv_cache, (k_new, v_new), num_tokens, q_len)
+        self._check(_marshal.kv_append_quantised(self._address(), self.config.max_blocks_per_seq, k_new, v_new, kv_cache, block_table,
+                                                 q_start, q_len, ctx_len, num_pages, num_tokens, self._workspace_or(workspace), stream))
+
+    def kv_read_quantised(self, kv_cache, block_table, q_start, q_len, ctx_len, k_rows, v_rows, num_pages: Optional[int] = None,
+                          num_tokens: Optional[int] = None, stream=None):
+        """``sarathi_kv_read_quantised``: what the cache holds of positions ctx_len - q_len .. ctx_len - 1, as rows."""
+        self._check_quantised(kv_cache, (k_rows, v_rows), num_tokens, q_len)
+        self._check(_marshal.kv_read_quantised(self._address(), self.config.max_blocks_per_seq, kv_cache, block_table, q_start, q_len,
+                                               ctx_len, num_pages, num_tokens, k_rows, v_rows, stream))
+        return k_rows, v_rows
+
+    def hybrid_attention_quantised(self, q, kv_cache, block_table, q_start, q_len, ctx_len, sm_scale: float, out,
+                                   num_pages: Optional[int] = None, num_tokens: Optional[int] = None, workspace=None, stream=None):
+        """``sarathi_hybrid_attention_quantised``: ``hybrid_attention`` over the 4-bit cache."""
+        self._check_quantised(kv_cache)
+        self._check(_marshal.attention_quantised(self._address(), self.config.max_blocks_per_seq, q, kv_cache, block_table, q_start, q_len,
+                                                 ctx_len, num_pages, num_tokens, float(sm_scale), out, stream, self._workspace_or(workspace)))
+        return out
+
+    def hybrid_attention_quantised_noalloc(self, q, kv_cache, block_table, q_start, q_len, ctx_len, sm_scale: float, out,
+                                           num_pages: Optional[int] = None, num_tokens: Optional[int] = None, stream=None):
+        """``sarathi_hybrid_attention_quantised_noalloc``: no workspace, the library's built-in scratch."""
+        self._check_quantised(kv_cache)
+        self._check(_marshal.attention_quantised(self._address(), self.config.max_blocks_per_seq, q, kv_cache, block_table, q_start, q_len,
+                                                 ctx_len, num_pages, num_tokens, float(sm_scale), out, stream))
         return out
 
 

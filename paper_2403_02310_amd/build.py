@@ -11,7 +11,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsarathi.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
-SOURCES = ["api.cpp", "linear_api.cpp", "plan.cpp", "scheduler.cpp", "attn_kernels.hip", "linear_kernels.hip"]
+SOURCES = ["api.cpp", "linear_api.cpp", "plan.cpp", "scheduler.cpp", "attn_kernels.hip", "quantised_kernels.hip", "linear_kernels.hip"]
 
 
 def build_library(verbose: bool = False) -> str:
@@ -40,10 +40,11 @@ def build_marshal() -> str:
     return MARSHAL
 
 
-def build_sanitized_host(out_dir: str) -> str:
+def build_sanitized_host(out_dir: str, driver: str = "host_paths.cpp") -> str:
     """CPU-only build for AddressSanitizer + UndefinedBehaviorSanitizer: the host translation units of the library
     (validation, planner, scheduler, entry-point bookkeeping) against stand-ins for the HIP runtime and the kernel
-    launchers, plus the fp64 checker's C sources, linked with the driver tests/sanitize/host_paths.cpp.
+    launchers, plus the fp64 checker's C sources, linked with a driver of tests/sanitize (host_paths.cpp does not call the 4-bit cache,
+    whose launchers it gets from a file of their own; quantised_paths.cpp brings them along).
     Nothing of it runs on a GPU.  Returns the path of the executable."""
     san = ["-fsanitize=address,undefined", "-fno-sanitize-recover=undefined", "-fno-omit-frame-pointer", "-g", "-O1"]
     inc = ["-I", os.path.join(ROOT, "include"), "-I", CSRC, "-I", "/opt/rocm/include", "-D__HIP_PLATFORM_AMD__"]
@@ -52,8 +53,9 @@ def build_sanitized_host(out_dir: str) -> str:
         obj = os.path.join(out_dir, src + ".o")
         subprocess.run(["gcc", "-std=c11", "-fopenmp", "-Wall", "-Wextra"] + san + ["-c", os.path.join(ROOT, "oracle", src), "-o", obj], check=True)
         objs.append(obj)
-    exe = os.path.join(out_dir, "host_paths_sanitized")
-    cpp = [os.path.join(CSRC, s) for s in ("api.cpp", "plan.cpp", "scheduler.cpp")] + [os.path.join(ROOT, "tests", "sanitize", "host_paths.cpp")]
+    exe = os.path.join(out_dir, driver.replace(".cpp", "_sanitized"))
+    drivers = ["host_paths.cpp", "quantised_launchers.cpp"] if driver == "host_paths.cpp" else [driver]
+    cpp = [os.path.join(CSRC, s) for s in ("api.cpp", "plan.cpp", "scheduler.cpp")] + [os.path.join(ROOT, "tests", "sanitize", d) for d in drivers]
     res = subprocess.run(["g++", "-std=c++17", "-Wall", "-Wextra", "-Wno-unused-parameter", "-fopenmp", "-static-libasan"] + san + inc + cpp + objs +
                          ["-o", exe, "-lm"], capture_output=True, text=True)
     if res.returncode != 0:

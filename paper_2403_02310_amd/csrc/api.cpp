@@ -48,6 +48,7 @@ struct sarathi_handle {
     void *resident_ws = nullptr;
     void *resident_stream = nullptr;
     std::vector<int32_t> resident_desc;  // q_len | ctx_len of the planned batch
+    bool resident_quantised = false;     // planned for the 4-bit cache
     uint64_t resident_opt_version = 0;
     uint64_t opt_version = 1;
     size_t resident_attn_off = 0;        // byte offset of the attention metadata inside the region
@@ -186,9 +187,15 @@ void pack_attn_meta(char *dst, const Plan &pl, const AttnMetaOffsets &o) {
     copy_vector(dst + o.reduce, pl.reduce_units);
 }
 
-bool resident_plan_matches(const sarathi_handle *h, const int32_t *q_len, const int32_t *ctx_len, int32_t n,
+// The cache of a call: two pools of bf16 pages, or one of 4-bit records.
+struct Cache {
+    const void *k, *v;
+    bool quantised;
+};
+
+bool resident_plan_matches(const sarathi_handle *h, bool quantised, const int32_t *q_len, const int32_t *ctx_len, int32_t n,
                            const void *workspace, const void *stream) {
-    if (h->resident_ws != workspace || h->resident_stream != stream || h->resident_opt_version != h->opt_version) return false;
+    if (h->resident_ws != workspace || h->resident_quantised != quantised || h->resident_stream != stream || h->resident_opt_version != h->opt_version) return false;
     if (h->resident_desc.size() != 2 * (size_t)n) return false;
     return std::memcmp(h->resident_desc.data(), q_len, sizeof(int32_t) * (size_t)n) == 0 &&
            std::memcmp(h->resident_desc.data() + n, ctx_len, sizeof(int32_t) * (size_t)n) == 0;
@@ -221,7 +228,7 @@ Schedule schedule_of(const sarathi_handle *h) {
     }
     const bool one_launch = chunk_blocks > 0 && wave_blocks > 0 && h->opt.interleave != 0;
     // The time the decodes need to stream their keys and values, and the longest block next to a chunk block.
-    const double key_us = h->cfg.head_dim * 4.0;
+    const double key_us = pl.key_bytes;
     const double wave_us = (double)pl.wave_keys * h->cfg.num_kv_heads * key_us / 6.5e6, longest_us = (double)pl.longest_wave_keys * key_us / kNextToChunks;
     const bool shared = 2 * pl.shared_wave_keys > pl.wave_keys;
     if (one_launch)
@@ -250,8 +257,8 @@ Schedule schedule_of(const sarathi_handle *h) {
 // second stream (both create runtime objects on first use).
 // `in_arguments`: `dev` is host memory instead, and the plan travels in the attention launch's arguments.
 sarathi_status enqueue_attention(sarathi_handle *h, char *dev, bool in_arguments, float *part_ml, float *part_o, int32_t *sched,
-                                 const int32_t *block_table, const void *q, const void *k_cache, const void *v_cache,
-                                 int64_t num_pages, float sm_scale, void *out, hipStream_t s, bool instrumented, bool sched_clear) {
+                                 const int32_t *block_table, const void *q, const Cache &cache, int64_t num_pages, float sm_scale, void *out,
+                                 hipStream_t s, bool instrumented, bool sched_clear) {
     const Plan &pl = h->plan;
     const AttnMetaOffsets mo = attn_meta_offsets(pl);
     const size_t units_off = mo.units, reduce_off = mo.reduce;
@@ -301,22 +308,26 @@ sarathi_status enqueue_attention(sarathi_handle *h, char *dev, bool in_arguments
         if (e == hipSuccess) e = hipEventCreateWithFlags(&h->join_event, hipEventDisableTiming);
         if (e != hipSuccess) return hip_fail(h, "hipEventCreate(fork/join)", e);
     }
+    auto attend = [&](int which, void *on) {
+        return (hipError_t)(cache.quantised ? launch_attention_quantised(h->cfg, m, q, cache.k, num_pages, sm_scale, out, which, on)
+                                            : launch_attention(h->cfg, m, q, cache.k, cache.v, num_pages, sm_scale, out, which, on));
+    };
     int32_t merged_on_side = 0;
     const int t1 = instrumented ? timing_begin(h, 1, s) : -1;
     if (fork) {
         e = hipEventRecord(h->fork_event, s);
         if (e == hipSuccess) e = hipStreamWaitEvent(h->side_stream, h->fork_event, 0);
         if (e != hipSuccess) return hip_fail(h, "fork to side stream", e);
-        e = (hipError_t)launch_attention(h->cfg, m, q, k_cache, v_cache, num_pages, sm_scale, out, 1, h->side_stream);
+        e = attend(1, h->side_stream);
         if (e == hipSuccess) e = (hipError_t)launch_reduce(h->cfg, m, out, 0, m.num_tile_reduce_units, h->side_stream);
         merged_on_side = m.num_tile_reduce_units;
         if (e == hipSuccess) e = hipEventRecord(h->join_event, h->side_stream);
-        if (e == hipSuccess) e = (hipError_t)launch_attention(h->cfg, m, q, k_cache, v_cache, num_pages, sm_scale, out, 2, stream);
+        if (e == hipSuccess) e = attend(2, stream);
         if (e == hipSuccess) e = hipStreamWaitEvent(s, h->join_event, 0);
     } else if (both && h->opt.interleave != 0) {  // one launch (also where the second stream is not to be used)
-        e = (hipError_t)launch_attention(h->cfg, m, q, k_cache, v_cache, num_pages, sm_scale, out, sched_plan.roles ? 5 : 4, stream);
+        e = attend(sched_plan.roles ? 5 : 4, stream);
     } else {
-        e = (hipError_t)launch_attention(h->cfg, m, q, k_cache, v_cache, num_pages, sm_scale, out, 3, stream);
+        e = attend(3, stream);
     }
     timing_end(h, 1, t1, s);
     if (e != hipSuccess) return hip_fail(h, "launch attention", e);
@@ -519,25 +530,10 @@ extern "C" sarathi_status sarathi_plan_hybrid_attention(sarathi_handle *h, const
     return SARATHI_OK;
 }
 
-extern "C" sarathi_status sarathi_kv_append(sarathi_handle *h, const void *k_new, const void *v_new, void *k_cache,
-                                            void *v_cache, const int32_t *block_table, const int32_t *q_start,
-                                            const int32_t *q_len, const int32_t *ctx_len, int32_t num_seqs,
-                                            int32_t num_tokens, int64_t num_pages, void *workspace, void *stream) {
-    if (!h) return SARATHI_EINVAL;
-    sarathi_status st = validate_batch(h->cfg, q_start, q_len, ctx_len, num_seqs, num_tokens, num_pages, h->err);
-    if (st != SARATHI_OK) return st;
-    if (num_seqs == 0) return SARATHI_OK;
-    if (!k_new || !v_new || !k_cache || !v_cache || !block_table) return fail(h, SARATHI_EINVAL, "null tensor pointer");
-    if (!workspace) return fail(h, SARATHI_EWORKSPACE, "null workspace");
-    if (reinterpret_cast<uintptr_t>(workspace) % 256 != 0) return fail(h, SARATHI_EWORKSPACE, "workspace is not 256-byte aligned");
-    if ((st = ensure_staging(h)) != SARATHI_OK) return st;
-    int slot;
-    if ((st = acquire_slot(h, static_cast<hipStream_t>(stream), &slot)) != SARATHI_OK) return st;
-    SlotGuard guard{h, slot, static_cast<hipStream_t>(stream)};
+namespace {
 
-    // Metadata: one record per cache page that this iteration writes into.
-    AppendUnit *units = static_cast<AppendUnit *>(h->staging[slot]);
-    const size_t n = (size_t)num_seqs;
+// One record per cache page that the batch's new positions lie in.
+size_t page_units(AppendUnit *units, const int32_t *q_start, const int32_t *q_len, const int32_t *ctx_len, int32_t num_seqs) {
     size_t n_units = 0;
     for (int32_t i = 0; i < num_seqs; ++i) {
         const int32_t prefix = ctx_len[i] - q_len[i];
@@ -546,13 +542,34 @@ extern "C" sarathi_status sarathi_kv_append(sarathi_handle *h, const void *k_new
             units[n_units++] = AppendUnit{i, pg, q_start[i] + (first - prefix), (first - pg * kPageSize) | ((end - pg * kPageSize) << 8)};
         }
     }
+    return n_units;
+}
+
+sarathi_status append_rows(sarathi_handle *h, const void *k_new, const void *v_new, void *k_cache, void *v_cache, bool quantised,
+                           const int32_t *block_table, const int32_t *q_start, const int32_t *q_len, const int32_t *ctx_len, int32_t num_seqs,
+                           int32_t num_tokens, int64_t num_pages, void *workspace, void *stream) {
+    if (!h) return SARATHI_EINVAL;
+    sarathi_status st = validate_batch(h->cfg, q_start, q_len, ctx_len, num_seqs, num_tokens, num_pages, h->err);
+    if (st != SARATHI_OK) return st;
+    if (num_seqs == 0) return SARATHI_OK;
+    if (!k_new || !v_new || !k_cache || (!v_cache && !quantised) || !block_table) return fail(h, SARATHI_EINVAL, "null tensor pointer");
+    if (!workspace) return fail(h, SARATHI_EWORKSPACE, "null workspace");
+    if (reinterpret_cast<uintptr_t>(workspace) % 256 != 0) return fail(h, SARATHI_EWORKSPACE, "workspace is not 256-byte aligned");
+    if ((st = ensure_staging(h)) != SARATHI_OK) return st;
+    int slot;
+    if ((st = acquire_slot(h, static_cast<hipStream_t>(stream), &slot)) != SARATHI_OK) return st;
+    SlotGuard guard{h, slot, static_cast<hipStream_t>(stream)};
+
+    AppendUnit *units = static_cast<AppendUnit *>(h->staging[slot]);
+    const size_t n = (size_t)num_seqs;
+    const size_t n_units = page_units(units, q_start, q_len, ctx_len, num_seqs);
     size_t used = sizeof(AppendUnit) * n_units;
     if (used > h->staging_bytes) return fail(h, SARATHI_ECAPACITY, "internal: metadata exceeds staging buffer");
     // The attention call of this iteration will get the same description: plan it now and let
     // its metadata ride along in the append launch (no host-to-device copy of its own).
     h->resident_ws = nullptr;
     if (h->opt.plan_at_append) {
-        plan_attention(h->cfg, h->opt, h->ws, q_start, q_len, ctx_len, num_seqs, h->plan);
+        plan_attention(h->cfg, h->opt, h->ws, q_start, q_len, ctx_len, num_seqs, h->plan, quantised);
         const AttnMetaOffsets o = attn_meta_offsets(h->plan);
         const size_t attn_off = align_up(used, 256);
         if (attn_off + o.total <= h->staging_bytes) {
@@ -564,6 +581,7 @@ extern "C" sarathi_status sarathi_kv_append(sarathi_handle *h, const void *k_new
             std::memcpy(h->resident_desc.data() + n, ctx_len, sizeof(int32_t) * n);
             h->resident_opt_version = h->opt_version;
             h->resident_stream = stream;
+            h->resident_quantised = quantised;
             h->resident_ws = workspace;
         }
     }
@@ -587,24 +605,22 @@ extern "C" sarathi_status sarathi_kv_append(sarathi_handle *h, const void *k_new
         h->resident_sched_clear = true;
     }
     const int t0 = timing_begin(h, 0, s);
-    hipError_t e = (hipError_t)launch_kv_append(h->cfg, m, k_new, v_new, k_cache, v_cache, num_pages, stream);
+    hipError_t e = (hipError_t)(quantised ? launch_kv_append_quantised(h->cfg, m, k_new, v_new, k_cache, num_pages, stream)
+                                          : launch_kv_append(h->cfg, m, k_new, v_new, k_cache, v_cache, num_pages, stream));
     timing_end(h, 0, t0, s);
     if (e != hipSuccess) { h->resident_ws = nullptr; return hip_fail(h, "launch kv_append", e); }
     if ((st = guard.release()) != SARATHI_OK) return st;
     return SARATHI_OK;
 }
 
-extern "C" sarathi_status sarathi_hybrid_attention(sarathi_handle *h, const void *q, const void *k_cache,
-                                                   const void *v_cache, const int32_t *block_table,
-                                                   const int32_t *q_start, const int32_t *q_len,
-                                                   const int32_t *ctx_len, int32_t num_seqs, int32_t num_tokens,
-                                                   int64_t num_pages, float sm_scale, void *out, void *workspace,
-                                                   void *stream) {
+sarathi_status attend(sarathi_handle *h, const void *q, const Cache &cache, const int32_t *block_table, const int32_t *q_start, const int32_t *q_len,
+                      const int32_t *ctx_len, int32_t num_seqs, int32_t num_tokens, int64_t num_pages, float sm_scale, void *out, void *workspace,
+                      void *stream) {
     if (!h) return SARATHI_EINVAL;
     sarathi_status st = validate_batch(h->cfg, q_start, q_len, ctx_len, num_seqs, num_tokens, num_pages, h->err);
     if (st != SARATHI_OK) return st;
     if (num_seqs == 0) return SARATHI_OK;
-    if (!q || !k_cache || !v_cache || !block_table || !out) return fail(h, SARATHI_EINVAL, "null tensor pointer");
+    if (!q || !cache.k || (!cache.v && !cache.quantised) || !block_table || !out) return fail(h, SARATHI_EINVAL, "null tensor pointer");
     if (!(sm_scale > 0.0f) || sm_scale - sm_scale != 0.0f) return fail(h, SARATHI_EINVAL, "sm_scale must be positive and finite");
     if (!workspace) return fail(h, SARATHI_EWORKSPACE, "null workspace");
     if (reinterpret_cast<uintptr_t>(workspace) % 256 != 0) return fail(h, SARATHI_EWORKSPACE, "workspace is not 256-byte aligned");
@@ -613,13 +629,13 @@ extern "C" sarathi_status sarathi_hybrid_attention(sarathi_handle *h, const void
     hipError_t e;
     char *dev;
     bool sched_clear = false;
-    if (resident_plan_matches(h, q_len, ctx_len, num_seqs, workspace, stream)) {
+    if (resident_plan_matches(h, cache.quantised, q_len, ctx_len, num_seqs, workspace, stream)) {
         // planned and uploaded by the sarathi_kv_append of this iteration (h->plan is that plan)
         dev = ws + h->ws.meta + h->resident_attn_off;
         sched_clear = h->resident_sched_clear;
         h->resident_sched_clear = false;
     } else {
-        plan_attention(h->cfg, h->opt, h->ws, q_start, q_len, ctx_len, num_seqs, h->plan);
+        plan_attention(h->cfg, h->opt, h->ws, q_start, q_len, ctx_len, num_seqs, h->plan, cache.quantised);
         if ((st = ensure_staging(h)) != SARATHI_OK) return st;
         int slot;
         if ((st = acquire_slot(h, s, &slot)) != SARATHI_OK) return st;
@@ -635,20 +651,17 @@ extern "C" sarathi_status sarathi_hybrid_attention(sarathi_handle *h, const void
         if ((st = guard.release()) != SARATHI_OK) return st;
     }
     return enqueue_attention(h, dev, false, reinterpret_cast<float *>(ws + h->ws.part_ml), reinterpret_cast<float *>(ws + h->ws.part_o),
-                             reinterpret_cast<int32_t *>(ws + h->ws.sched), block_table, q, k_cache, v_cache, num_pages, sm_scale,
-                             out, s, /*instrumented=*/true, sched_clear);
+                             reinterpret_cast<int32_t *>(ws + h->ws.sched), block_table, q, cache, num_pages, sm_scale, out, s, /*instrumented=*/true, sched_clear);
 }
 
-extern "C" sarathi_status sarathi_hybrid_attention_noalloc(sarathi_handle *h, const void *q, const void *k_cache,
-                                                           const void *v_cache, const int32_t *block_table,
-                                                           const int32_t *q_start, const int32_t *q_len,
-                                                           const int32_t *ctx_len, int32_t num_seqs, int32_t num_tokens,
-                                                           int64_t num_pages, float sm_scale, void *out, void *stream) {
+sarathi_status attend_noalloc(sarathi_handle *h, const void *q, const Cache &cache, const int32_t *block_table, const int32_t *q_start,
+                              const int32_t *q_len, const int32_t *ctx_len, int32_t num_seqs, int32_t num_tokens, int64_t num_pages, float sm_scale,
+                              void *out, void *stream) {
     if (!h) return SARATHI_EINVAL;
     sarathi_status st = validate_batch(h->cfg, q_start, q_len, ctx_len, num_seqs, num_tokens, num_pages, h->err);
     if (st != SARATHI_OK) return st;
     if (num_seqs == 0) return SARATHI_OK;
-    if (!q || !k_cache || !v_cache || !block_table || !out) return fail(h, SARATHI_EINVAL, "null tensor pointer");
+    if (!q || !cache.k || (!cache.v && !cache.quantised) || !block_table || !out) return fail(h, SARATHI_EINVAL, "null tensor pointer");
     if (!(sm_scale > 0.0f) || sm_scale - sm_scale != 0.0f) return fail(h, SARATHI_EINVAL, "sm_scale must be positive and finite");
     // Partial rows and metadata the built-in scratch holds; the planner coarsens its splits until both fit.
     const size_t row_bytes = sizeof(float) * (size_t)h->cfg.num_kv_heads * h->cfg.head_dim;
@@ -659,7 +672,7 @@ extern "C" sarathi_status sarathi_hybrid_attention_noalloc(sarathi_handle *h, co
     lay.max_attn_meta = kStaticMetaBytes;
     lay.meta_per_launch = kUploadArgBytes;
     h->resident_ws = nullptr;  // h->plan is about to be overwritten
-    plan_attention(h->cfg, h->opt, lay, q_start, q_len, ctx_len, num_seqs, h->plan);
+    plan_attention(h->cfg, h->opt, lay, q_start, q_len, ctx_len, num_seqs, h->plan, cache.quantised);
     const AttnMetaOffsets o = attn_meta_offsets(h->plan);
     if (o.total > kStaticMetaBytes || o.total > h->noalloc_meta.size()) {
         char buf[200];
@@ -678,6 +691,98 @@ extern "C" sarathi_status sarathi_hybrid_attention_noalloc(sarathi_handle *h, co
         e = (hipError_t)launch_upload_args(sc.meta, h->noalloc_meta.data(), o.total, stream);
         if (e != hipSuccess) return hip_fail(h, "launch upload(metadata in kernel arguments)", e);
     }
-    return enqueue_attention(h, with_launch ? h->noalloc_meta.data() : sc.meta, with_launch, sc.part_ml, sc.part_o, sc.sched, block_table, q, k_cache, v_cache, num_pages, sm_scale,
-                             out, static_cast<hipStream_t>(stream), /*instrumented=*/false, /*sched_clear=*/false);
+    return enqueue_attention(h, with_launch ? h->noalloc_meta.data() : sc.meta, with_launch, sc.part_ml, sc.part_o, sc.sched, block_table, q, cache, num_pages, sm_scale, out,
+                             static_cast<hipStream_t>(stream), /*instrumented=*/false, /*sched_clear=*/false);
+}
+
+}  // namespace
+
+extern "C" sarathi_status sarathi_kv_append(sarathi_handle *h, const void *k_new, const void *v_new, void *k_cache,
+                                            void *v_cache, const int32_t *block_table, const int32_t *q_start,
+                                            const int32_t *q_len, const int32_t *ctx_len, int32_t num_seqs,
+                                            int32_t num_tokens, int64_t num_pages, void *workspace, void *stream) {
+    return append_rows(h, k_new, v_new, k_cache, v_cache, false, block_table, q_start, q_len, ctx_len, num_seqs, num_tokens, num_pages, workspace,
+                       stream);
+}
+
+extern "C" sarathi_status sarathi_hybrid_attention(sarathi_handle *h, const void *q, const void *k_cache,
+                                                   const void *v_cache, const int32_t *block_table,
+                                                   const int32_t *q_start, const int32_t *q_len,
+                                                   const int32_t *ctx_len, int32_t num_seqs, int32_t num_tokens,
+                                                   int64_t num_pages, float sm_scale, void *out, void *workspace,
+                                                   void *stream) {
+    return attend(h, q, Cache{k_cache, v_cache, false}, block_table, q_start, q_len, ctx_len, num_seqs, num_tokens, num_pages, sm_scale, out, workspace,
+                  stream);
+}
+
+extern "C" sarathi_status sarathi_hybrid_attention_noalloc(sarathi_handle *h, const void *q, const void *k_cache,
+                                                           const void *v_cache, const int32_t *block_table,
+                                                           const int32_t *q_start, const int32_t *q_len,
+                                                           const int32_t *ctx_len, int32_t num_seqs, int32_t num_tokens,
+                                                           int64_t num_pages, float sm_scale, void *out, void *stream) {
+    return attend_noalloc(h, q, Cache{k_cache, v_cache, false}, block_table, q_start, q_len, ctx_len, num_seqs, num_tokens, num_pages, sm_scale, out,
+                          stream);
+}
+
+// ---- the same over the 4-bit cache ----
+
+extern "C" size_t sarathi_quantised_page_bytes(const sarathi_handle *h) {
+    return h ? quantised_record_bytes(h->cfg.head_dim) * (size_t)h->cfg.num_kv_heads : 0;
+}
+
+namespace {
+// Records are read and written 16 bytes at a time.
+bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+}  // namespace
+
+extern "C" sarathi_status sarathi_kv_append_quantised(sarathi_handle *h, const void *k_new, const void *v_new, void *kv_cache,
+                                                      const int32_t *block_table, const int32_t *q_start, const int32_t *q_len,
+                                                      const int32_t *ctx_len, int32_t num_seqs, int32_t num_tokens, int64_t num_pages,
+                                                      void *workspace, void *stream) {
+    if (h && !(aligned16(k_new) && aligned16(v_new) && aligned16(kv_cache))) return fail(h, SARATHI_EINVAL, "rows and kv_cache must be 16-byte aligned");
+    return append_rows(h, k_new, v_new, kv_cache, nullptr, true, block_table, q_start, q_len, ctx_len, num_seqs, num_tokens, num_pages, workspace,
+                       stream);
+}
+
+extern "C" sarathi_status sarathi_kv_read_quantised(sarathi_handle *h, const void *kv_cache, const int32_t *block_table, const int32_t *q_start,
+                                                    const int32_t *q_len, const int32_t *ctx_len, int32_t num_seqs, int32_t num_tokens,
+                                                    int64_t num_pages, void *k_rows, void *v_rows, void *stream) {
+    if (!h) return SARATHI_EINVAL;
+    sarathi_status st = validate_batch(h->cfg, q_start, q_len, ctx_len, num_seqs, num_tokens, num_pages, h->err);
+    if (st != SARATHI_OK) return st;
+    if (num_seqs == 0) return SARATHI_OK;
+    if (!kv_cache || !block_table || !k_rows || !v_rows) return fail(h, SARATHI_EINVAL, "null tensor pointer");
+    if (!(aligned16(kv_cache) && aligned16(k_rows) && aligned16(v_rows))) return fail(h, SARATHI_EINVAL, "rows and kv_cache must be 16-byte aligned");
+    if ((st = ensure_staging(h)) != SARATHI_OK) return st;
+    int slot;
+    if ((st = acquire_slot(h, static_cast<hipStream_t>(stream), &slot)) != SARATHI_OK) return st;
+    SlotGuard guard{h, slot, static_cast<hipStream_t>(stream)};
+    AppendUnit *units = static_cast<AppendUnit *>(h->staging[slot]);
+    AppendMeta m;
+    m.units = static_cast<const AppendUnit *>(h->staging_dev[slot]);
+    if (h->opt.inline_append) m.units_host = units;
+    m.block_table = block_table;
+    m.max_blocks = h->cfg.max_blocks_per_seq;
+    m.num_units = (int32_t)page_units(units, q_start, q_len, ctx_len, num_seqs);
+    const hipError_t e = (hipError_t)launch_kv_read_quantised(h->cfg, m, kv_cache, num_pages, k_rows, v_rows, stream);
+    if (e != hipSuccess) return hip_fail(h, "launch kv_read", e);
+    return guard.release();
+}
+
+extern "C" sarathi_status sarathi_hybrid_attention_quantised(sarathi_handle *h, const void *q, const void *kv_cache, const int32_t *block_table,
+                                                             const int32_t *q_start, const int32_t *q_len, const int32_t *ctx_len,
+                                                             int32_t num_seqs, int32_t num_tokens, int64_t num_pages, float sm_scale, void *out,
+                                                             void *workspace, void *stream) {
+    if (h && !aligned16(kv_cache)) return fail(h, SARATHI_EINVAL, "kv_cache must be 16-byte aligned");
+    return attend(h, q, Cache{kv_cache, nullptr, true}, block_table, q_start, q_len, ctx_len, num_seqs, num_tokens, num_pages, sm_scale, out, workspace,
+                  stream);
+}
+
+extern "C" sarathi_status sarathi_hybrid_attention_quantised_noalloc(sarathi_handle *h, const void *q, const void *kv_cache,
+                                                                     const int32_t *block_table, const int32_t *q_start, const int32_t *q_len,
+                                                                     const int32_t *ctx_len, int32_t num_seqs, int32_t num_tokens,
+                                                                     int64_t num_pages, float sm_scale, void *out, void *stream) {
+    if (h && !aligned16(kv_cache)) return fail(h, SARATHI_EINVAL, "kv_cache must be 16-byte aligned");
+    return attend_noalloc(h, q, Cache{kv_cache, nullptr, true}, block_table, q_start, q_len, ctx_len, num_seqs, num_tokens, num_pages, sm_scale, out,
+                          stream);
 }

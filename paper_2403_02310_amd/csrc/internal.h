@@ -83,6 +83,7 @@ struct Plan {
     int64_t shared_wave_keys = 0;     // those of sequences with several wave tiles, which read the same keys
     int32_t longest_wave_keys = 0;    // of the longest wave unit
     bool even_decode_pieces = false;  // few decodes, cut into pieces of nearly one length
+    double key_bytes = 0.0;           // of a position's key and value in the cache, one KV head
 };
 
 // Whether the blocks of a launch of both kinds of tile take their role at run time: `stream_us` is the time the decodes' keys and
@@ -157,7 +158,7 @@ sarathi_status validate_batch(const sarathi_config &cfg, const int32_t *q_start,
 // Work decomposition for sarathi_hybrid_attention.
 void plan_attention(const sarathi_config &cfg, const Options &opt, const WorkspaceLayout &ws,
                     const int32_t *q_start, const int32_t *q_len, const int32_t *ctx_len, int32_t num_seqs,
-                    Plan &plan);
+                    Plan &plan, bool quantised = false);
 
 // ---- device launchers (attn_kernels.hip); each returns a hipError_t cast to int ----
 // The append kernel's work item is a page unit: the slots [lo, hi) of ONE cache page that this
@@ -222,6 +223,16 @@ struct AttnMeta {
 // the chunk tiles' items), 5 = one launch in which one block per compute unit prefers chunk tiles (with queue_blocks)
 int launch_attention(const sarathi_config &cfg, const AttnMeta &m, const void *q, const void *k_cache,
                      const void *v_cache, int64_t num_pages, float sm_scale, void *out, int which, void *stream);
+
+// ---- the same over the 4-bit cache (quantised_kernels.hip) ----
+// Bytes of the record of a page and KV head: codes of the keys and of the values, the keys' scales, the values' scales.
+constexpr size_t quantised_record_bytes(int head_dim) { return (size_t)(16 * head_dim + head_dim / 2 + 4 * kPageSize); }
+int launch_kv_append_quantised(const sarathi_config &cfg, const AppendMeta &m, const void *k_new, const void *v_new, void *kv_cache,
+                               int64_t num_pages, void *stream);
+int launch_kv_read_quantised(const sarathi_config &cfg, const AppendMeta &m, const void *kv_cache, int64_t num_pages, void *k_rows, void *v_rows,
+                             void *stream);
+int launch_attention_quantised(const sarathi_config &cfg, const AttnMeta &m, const void *q, const void *kv_cache, int64_t num_pages,
+                               float sm_scale, void *out, int which, void *stream);
 
 // Merges the split tiles named by reduce_units[first .. first+count).
 // Fills `bytes` (a multiple of 4) at `ptr` with zeros by a small kernel (no memset node: callers may capture).

@@ -17,9 +17,22 @@ using AttentionFn = int (*)(void *, const void *, const void *, const void *, co
                             int32_t, int32_t, int64_t, float, void *, void *, void *);
 using NoallocFn = int (*)(void *, const void *, const void *, const void *, const int32_t *, const int32_t *, const int32_t *, const int32_t *,
                           int32_t, int32_t, int64_t, float, void *, void *);
+// the same over one pool of 4-bit records instead of two of bf16 pages
+using AppendQuantisedFn = int (*)(void *, const void *, const void *, void *, const int32_t *, const int32_t *, const int32_t *, const int32_t *, int32_t,
+                                  int32_t, int64_t, void *, void *);
+using ReadQuantisedFn = int (*)(void *, const void *, const int32_t *, const int32_t *, const int32_t *, const int32_t *, int32_t, int32_t, int64_t, void *,
+                                void *, void *);
+using AttentionQuantisedFn = int (*)(void *, const void *, const void *, const int32_t *, const int32_t *, const int32_t *, const int32_t *, int32_t,
+                                     int32_t, int64_t, float, void *, void *, void *);
+using NoallocQuantisedFn = int (*)(void *, const void *, const void *, const int32_t *, const int32_t *, const int32_t *, const int32_t *, int32_t, int32_t,
+                                   int64_t, float, void *, void *);
 AppendFn append_fn;
 AttentionFn attention_fn;
 NoallocFn noalloc_fn;
+AppendQuantisedFn append_quantised_fn;
+ReadQuantisedFn read_quantised_fn;
+AttentionQuantisedFn attention_quantised_fn;
+NoallocQuantisedFn noalloc_quantised_fn;
 // registered by binding.py, kept for the life of the process
 PyObject *ndarray_type, *as_i32, *current_stream, *refuse_table;
 PyObject *as_c_int32, *as_c_int64, *as_c_address;
@@ -223,6 +236,59 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return PyLong_FromLong(st);
 }
 
+// (handle, max_blocks, k_new, v_new, kv_cache, block_table, q_start, q_len, ctx_len, num_pages, num_tokens, workspace, stream)
+PyObject *kv_append_quantised(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (!arity(n, 13)) return nullptr;
+    void *h, *k_new, *v_new, *cache, *ws, *stream;
+    Batch b;
+    if (!device(a[0], &h) || !b.get(PyLong_AsLongLong(a[1]), a[5], a[6], a[7], a[8], a[9], a[10], a[4]) || !device(a[2], &k_new) ||
+        !device(a[3], &v_new) || !device(a[4], &cache) || !device(a[11], &ws) || !stream_of(a[12], &stream))
+        return nullptr;
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = append_quantised_fn(h, k_new, v_new, cache, static_cast<const int32_t *>(b.table), b.q_start.data(), b.q_len.data(), b.ctx_len.data(), b.num_seqs,
+                             b.num_tokens, b.num_pages, ws, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+}
+
+// (handle, max_blocks, kv_cache, block_table, q_start, q_len, ctx_len, num_pages, num_tokens, k_rows, v_rows, stream)
+PyObject *kv_read_quantised(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (!arity(n, 12)) return nullptr;
+    void *h, *cache, *k_rows, *v_rows, *stream;
+    Batch b;
+    if (!device(a[0], &h) || !b.get(PyLong_AsLongLong(a[1]), a[3], a[4], a[5], a[6], a[7], a[8], a[2]) || !device(a[2], &cache) ||
+        !device(a[9], &k_rows) || !device(a[10], &v_rows) || !stream_of(a[11], &stream))
+        return nullptr;
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = read_quantised_fn(h, cache, static_cast<const int32_t *>(b.table), b.q_start.data(), b.q_len.data(), b.ctx_len.data(), b.num_seqs, b.num_tokens,
+                           b.num_pages, k_rows, v_rows, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+}
+
+// (handle, max_blocks, q, kv_cache, block_table, q_start, q_len, ctx_len, num_pages, num_tokens, sm_scale, out, stream[, workspace]):
+// without a workspace the allocation-free call
+PyObject *attention_quantised(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 13 && !arity(n, 14)) return nullptr;
+    void *h, *q, *cache, *out, *stream, *ws = nullptr;
+    Batch b;
+    if (!device(a[0], &h) || !b.get(PyLong_AsLongLong(a[1]), a[4], a[5], a[6], a[7], a[8], a[9], a[3]) || !device(a[2], &q) || !device(a[3], &cache))
+        return nullptr;
+    const float scale = static_cast<float>(PyFloat_AsDouble(a[10]));
+    if (PyErr_Occurred() || !device(a[11], &out) || !stream_of(a[12], &stream) || (n == 14 && !device(a[13], &ws))) return nullptr;
+    const auto *table = static_cast<const int32_t *>(b.table);
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    if (n == 14)
+        st = attention_quantised_fn(h, q, cache, table, b.q_start.data(), b.q_len.data(), b.ctx_len.data(), b.num_seqs, b.num_tokens, b.num_pages, scale, out, ws, stream);
+    else
+        st = noalloc_quantised_fn(h, q, cache, table, b.q_start.data(), b.q_len.data(), b.ctx_len.data(), b.num_seqs, b.num_tokens, b.num_pages, scale, out, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+}
+
 void keep(PyObject **const *places, PyObject *const *objects, int n) {
     for (int i = 0; i < n; ++i) {
         Py_INCREF(objects[i]);
@@ -248,6 +314,19 @@ PyObject *setup(PyObject *, PyObject *const *a, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
+// (address of sarathi_kv_append_quantised, .._kv_read_quantised, .._hybrid_attention_quantised, .._hybrid_attention_quantised_noalloc)
+PyObject *setup_quantised(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (!arity(n, 4)) return nullptr;
+    void *f[4];
+    for (int i = 0; i < 4; ++i)
+        if (!as_address(a[i], &f[i])) return nullptr;
+    append_quantised_fn = reinterpret_cast<AppendQuantisedFn>(f[0]);
+    read_quantised_fn = reinterpret_cast<ReadQuantisedFn>(f[1]);
+    attention_quantised_fn = reinterpret_cast<AttentionQuantisedFn>(f[2]);
+    noalloc_quantised_fn = reinterpret_cast<NoallocQuantisedFn>(f[3]);
+    Py_RETURN_NONE;
+}
+
 // (as_c_int32, as_c_int64, as_c_address)
 PyObject *conversions(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (!arity(n, 3)) return nullptr;
@@ -259,6 +338,10 @@ PyObject *conversions(PyObject *, PyObject *const *a, Py_ssize_t n) {
 PyMethodDef methods[] = {
     {"kv_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(kv_append)), METH_FASTCALL, nullptr},
     {"attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(attention)), METH_FASTCALL, nullptr},
+    {"kv_append_quantised", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(kv_append_quantised)), METH_FASTCALL, nullptr},
+    {"kv_read_quantised", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(kv_read_quantised)), METH_FASTCALL, nullptr},
+    {"attention_quantised", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(attention_quantised)), METH_FASTCALL, nullptr},
+    {"setup_quantised", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(setup_quantised)), METH_FASTCALL, nullptr},
     {"conversions", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(conversions)), METH_FASTCALL, nullptr},
     {"setup", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(setup)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},

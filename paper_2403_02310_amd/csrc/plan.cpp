@@ -580,7 +580,7 @@ bool chunks_as_wave_tiles(const sarathi_config &cfg, const Options &opt, const W
 
 void plan_attention(const sarathi_config &cfg, const Options &opt, const WorkspaceLayout &ws,
                     const int32_t *q_start, const int32_t *q_len, const int32_t *ctx_len, int32_t num_seqs,
-                    Plan &plan) {
+                    Plan &plan, bool quantised) {
     plan.tiles.clear();
     plan.units.clear();
     plan.reduce_units.clear();
@@ -590,8 +590,9 @@ void plan_attention(const sarathi_config &cfg, const Options &opt, const Workspa
     plan.num_split_tiles = 0;
     plan.most_pieces = 0;
     plan.shared_wave_keys = 0;
+    plan.key_bytes = quantised ? (double)quantised_record_bytes(cfg.head_dim) / kPageSize : cfg.head_dim * 4.0;
     const int32_t G = cfg.num_q_heads / cfg.num_kv_heads;
-    int64_t min_cols = opt.tile_min_cols;
+    int64_t min_cols = quantised ? INT64_MAX : opt.tile_min_cols;
     if (min_cols <= 0) min_cols = chunks_as_wave_tiles(cfg, opt, ws, q_len, ctx_len, num_seqs) ? INT64_MAX : kChunkMinCols;
 
     // Tiles: chunk tiles first, then wave tiles (two passes keep each kind contiguous).

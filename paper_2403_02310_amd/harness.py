@@ -148,3 +148,44 @@ def setup_and_run(batch: HybridBatch, poison: Optional[int] = POISON_NAN, handle
     torch.cuda.synchronize()
     return {"handle": handle, "k_cache": k_cache, "v_cache": v_cache, "bt": bt_dev, "q": q_dev, "out": out,
             "kv_host": kv_host}
+
+
+# ---- the same over the 4-bit cache ---------------------------------------------------------
+
+def make_quantised_pool(handle: binding.Handle, num_pages: int, fill: int = 0xFF, device="cuda") -> torch.Tensor:
+    """A pool whose every byte is ``fill`` (0xFF: scales that are NaN)."""
+    return torch.full(handle.quantised_cache_shape(num_pages), fill, dtype=torch.uint8, device=device)
+
+
+def run_iteration_quantised(handle, batch: HybridBatch, pool, bt_dev, q_dev, k_new_dev, v_new_dev, out_dev=None):
+    """One iteration over the 4-bit cache: append the new K/V rows, then attention over the batch."""
+    if out_dev is None:
+        out_dev = torch.empty_like(q_dev)
+    handle.kv_append_quantised(k_new_dev, v_new_dev, pool, bt_dev, batch.q_start, batch.q_len, batch.ctx_len)
+    handle.hybrid_attention_quantised(q_dev, pool, bt_dev, batch.q_start, batch.q_len, batch.ctx_len, batch.sm_scale, out_dev)
+    return out_dev
+
+
+class _OnePool:
+    """A handle whose ``kv_append`` takes the 4-bit pool where the two bf16 pools go (for ``append_ranges``)."""
+
+    def __init__(self, handle: binding.Handle):
+        self.config, self._append = handle.config, handle.kv_append_quantised
+
+    def kv_append(self, k_new, v_new, pool, _, block_table, q_start, q_len, ctx_len):
+        self._append(k_new, v_new, pool, block_table, q_start, q_len, ctx_len)
+
+
+def setup_and_run_quantised(batch: HybridBatch, fill: int = 0xFF, handle=None, kv_host: Optional[dict] = None,
+                            q_bits: Optional[np.ndarray] = None):
+    """``setup_and_run`` over the 4-bit cache, on a fresh pool of ``fill`` bytes."""
+    handle = handle or make_handle(batch)
+    pool = make_quantised_pool(handle, batch.num_pages, fill)
+    bt_dev = torch.from_numpy(batch.block_table).cuda()
+    kv_host = {} if kv_host is None else kv_host
+    fill_prefixes(_OnePool(handle), batch, pool, None, bt_dev, kv_host)
+    k_new, v_new = (bits_to_device(x) for x in new_token_kv(batch, kv_host))
+    q_dev = bits_to_device(batch.q_bits(0) if q_bits is None else q_bits)
+    out = run_iteration_quantised(handle, batch, pool, bt_dev, q_dev, k_new, v_new)
+    torch.cuda.synchronize()
+    return {"handle": handle, "pool": pool, "bt": bt_dev, "q": q_dev, "out": out, "kv_host": kv_host, "k_new": k_new, "v_new": v_new}

@@ -1,0 +1,123 @@
+"""CPU tests of the 4-bit cache's entry points: sizes, refusals, marshalling, and the host code under sanitizers."""
+import os
+import subprocess
+
+import numpy as np
+import pytest
+
+from paper_2403_02310_amd import binding, build
+
+QS, QL, CL = [0, 3], [3, 1], [20, 33]
+
+
+class Tensor:
+    """What the binding looks at of a device tensor."""
+
+    def __init__(self, shape, item, address=4096, contiguous=True):
+        self.shape, self.item, self.address, self.contiguous = shape, item, address, contiguous
+
+    def is_contiguous(self):
+        return self.contiguous
+
+    def data_ptr(self):
+        return self.address
+
+    def element_size(self):
+        return self.item
+
+
+def _handle(d=128, heads=2):
+    return binding.Handle(8, heads, d, max_tokens=64, max_seqs=4, max_blocks_per_seq=4)
+
+
+def _args(d=128, heads=2):
+    return {"cache": Tensor((9, heads, 16 * d + d // 2 + 64), 1), "table": Tensor((2, 4), 4), "k": Tensor((4, heads, d), 2), "v": Tensor((4, heads, d), 2),
+            "q": Tensor((4, 8, d), 2), "out": Tensor((4, 8, d), 2), "ws": 256, "pages": None, "tokens": None, "scale": 0.5}
+
+
+def _calls(h, a, lengths=(QS, QL, CL)):
+    more = dict(num_pages=a["pages"], num_tokens=a["tokens"], stream=7)
+    return {
+        "append": lambda: h.kv_append_quantised(a["k"], a["v"], a["cache"], a["table"], *lengths, workspace=a["ws"], **more),
+        "read": lambda: h.kv_read_quantised(a["cache"], a["table"], *lengths, a["k"], a["v"], **more),
+        "attend": lambda: h.hybrid_attention_quantised(a["q"], a["cache"], a["table"], *lengths, a["scale"], a["out"], workspace=a["ws"], **more),
+        "noalloc": lambda: h.hybrid_attention_quantised_noalloc(a["q"], a["cache"], a["table"], *lengths, a["scale"], a["out"], **more),
+    }
+
+
+@pytest.mark.parametrize("d,heads,record", [(128, 2, 2176), (64, 1, 1120), (128, 8, 2176)])
+def test_cache_shape(d, heads, record):
+    h = binding.Handle(8, heads, d, max_tokens=64, max_seqs=4, max_blocks_per_seq=4)
+    assert h.quantised_cache_shape(11) == (11, heads, record)
+    assert binding.lib.sarathi_quantised_page_bytes(h._h) == heads * record
+
+
+@pytest.mark.parametrize("call", ["append", "read", "attend", "noalloc"])
+def test_batches_are_refused_before_anything_is_enqueued(call):
+    h = _handle()
+    for lengths, status in (((QS, [3, 0], CL), binding.EINVAL), ((QS, QL, [2, 33]), binding.EINVAL), (([1, 3], QL, CL), binding.EINVAL),
+                            ((QS, QL, [20, 65]), binding.ECAPACITY)):
+        with pytest.raises(binding.SarathiError) as e:
+            _calls(h, {**_args(), "tokens": 4}, lengths)[call]()
+        assert e.value.status == status
+    for change, status in (({"pages": 0}, binding.EINVAL), ({"tokens": 3}, binding.EINVAL), ({"cache": 0, "pages": 9}, binding.EINVAL),
+                           ({"cache": 4104, "pages": 9}, binding.EINVAL), ({"table": 0}, binding.EINVAL), ({"tokens": -1}, binding.EINVAL)):
+        with pytest.raises(binding.SarathiError) as e:
+            _calls(h, {**_args(), **change})[call]()
+        assert e.value.status == status, change
+
+
+@pytest.mark.parametrize("call,change", [
+    ("append", {"k": 0}), ("append", {"v": 0}), ("append", {"k": 4098}), ("read", {"k": 0}), ("read", {"v": 4104}), ("attend", {"q": 0}),
+    ("attend", {"out": 0}), ("attend", {"scale": 0.0}), ("attend", {"scale": float("nan")}), ("noalloc", {"scale": float("inf")}), ("noalloc", {"out": 0})])
+def test_tensors_and_scales_are_refused(call, change):
+    with pytest.raises(binding.SarathiError) as e:
+        _calls(_handle(), {**_args(), **change})[call]()
+    assert e.value.status == binding.EINVAL
+
+
+@pytest.mark.parametrize("call", ["append", "attend"])
+def test_workspaces_are_refused(call):
+    for ws in (0, 128):
+        with pytest.raises(binding.SarathiError) as e:
+            _calls(_handle(), {**_args(), "ws": ws})[call]()
+        assert e.value.status == binding.EWORKSPACE
+
+
+@pytest.mark.parametrize("call", ["append", "read", "attend", "noalloc"])
+@pytest.mark.parametrize("cache", [Tensor((9, 2, 2175), 1), Tensor((9, 1, 2176), 1), Tensor((9, 2, 2176), 2), Tensor((9, 4352), 1),
+                                   Tensor((9, 2, 2176), 1, contiguous=False)])
+def test_pools_of_another_shape_are_refused(call, cache):
+    with pytest.raises(ValueError):
+        _calls(_handle(), {**_args(), "cache": cache})[call]()
+
+
+@pytest.mark.parametrize("call", ["append", "read"])
+@pytest.mark.parametrize("rows", [Tensor((3, 2, 128), 2), Tensor((4, 2, 64), 2), Tensor((4, 8, 128), 2), Tensor((4, 2, 128), 4), Tensor((4, 256), 2),
+                                  Tensor((4, 2, 128), 2, contiguous=False)])
+def test_rows_of_another_shape_are_refused(call, rows):
+    with pytest.raises(ValueError):
+        _calls(_handle(), {**_args(), "v": rows})[call]()
+
+
+@pytest.mark.parametrize("call", ["append", "read", "attend", "noalloc"])
+def test_tables_and_length_arrays_are_refused_as_for_the_other_cache(call):
+    for change in ({"table": Tensor((2, 5), 4)}, {"table": Tensor((1, 4), 4)}):
+        with pytest.raises(ValueError):
+            _calls(_handle(), {**_args(), **change})[call]()
+    with pytest.raises(ValueError):
+        _calls(_handle(), _args(), (QS, QL, CL[:1]))[call]()
+
+
+def test_an_empty_batch_enqueues_nothing():
+    for call in _calls(_handle(), {**_args(), "pages": 9}, (np.zeros(0, np.int32),) * 3).values():
+        call()
+
+
+def test_host_paths_are_clean_under_asan_and_ubsan(tmp_path):
+    exe = build.build_sanitized_host(str(tmp_path), "quantised_paths.cpp")
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=1:abort_on_error=0:halt_on_error=1", UBSAN_OPTIONS="halt_on_error=1:print_stacktrace=1")
+    res = subprocess.run([exe], capture_output=True, text=True, timeout=600, env=env)
+    assert res.returncode == 0, res.stdout[-2000:] + res.stderr[-6000:]
+    assert "quantised paths clean" in res.stdout
+    assert "ERROR: AddressSanitizer" not in res.stderr and "runtime error" not in res.stderr, res.stderr[-6000:]
