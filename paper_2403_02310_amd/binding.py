@@ -223,6 +223,8 @@ class Handle:
             raise SarathiError(st, "sarathi_create rejected the configuration")
         self._h = h
         self.workspace = None
+        # block table, KV heads, channels and record of the 4-bit cache, for the calls that check its tensors
+        self._widths = (max_blocks_per_seq, num_kv_heads, head_dim, int(lib.sarathi_quantised_page_bytes(h)) // num_kv_heads)
 
     def close(self):
         if getattr(self, "_h", None):
@@ -308,51 +310,32 @@ class Handle:
     # ---- the same over the 4-bit cache -----------------------------------
     def quantised_cache_shape(self, num_pages: int) -> tuple:
         """Shape of the uint8 pool of the 4-bit cache: a record for each page and KV head."""
-        heads = self.config.num_kv_heads
-        return num_pages, heads, int(lib.sarathi_quantised_page_bytes(self._h)) // heads
-
-    def _check_quantised(self, kv_cache, rows=(), num_tokens: Optional[int] = None, q_len=()) -> None:
-        """The C ABI takes bare pointers; a pool or rows of another shape or type would be walked with the handle's."""
-        shape = getattr(kv_cache, "shape", None)
-        if shape is not None and (len(shape) != 3 or kv_cache.element_size() != 1 or tuple(shape) != self.quantised_cache_shape(int(shape[0]))):
-            raise ValueError("kv_cache must be bytes of shape %s, got %s of %s"
-                             % (("pages",) + self.quantised_cache_shape(0)[1:], tuple(shape), getattr(kv_cache, "dtype", None)))
-        for r in rows:
-            shape = getattr(r, "shape", None)
-            if shape is None:
-                continue
-            want = int(np.sum(q_len)) if num_tokens is None else num_tokens
-            if len(shape) != 3 or tuple(shape[1:]) != (self.config.num_kv_heads, self.config.head_dim) or int(shape[0]) < want or r.element_size() != 2:
-                raise ValueError("rows must be bf16 [>= %d, %d, %d], got %s" % (want, self.config.num_kv_heads, self.config.head_dim, tuple(shape)))
+        return num_pages, self._widths[1], self._widths[3]
 
     def kv_append_quantised(self, k_new, v_new, kv_cache, block_table, q_start, q_len, ctx_len, num_pages: Optional[int] = None,
                             num_tokens: Optional[int] = None, workspace=None, stream=None):
         """``sarathi_kv_append_quantised``: the new rows in 4 bits into ``kv_cache``, uint8 of ``quantised_cache_shape``."""
-        self._check_quantised(kv_cache, (k_new, v_new), num_tokens, q_len)
-        self._check(_marshal.kv_append_quantised(self._address(), self.config.max_blocks_per_seq, k_new, v_new, kv_cache, block_table,
+        self._check(_marshal.kv_append_quantised(self._address(), *self._widths, k_new, v_new, kv_cache, block_table,
                                                  q_start, q_len, ctx_len, num_pages, num_tokens, self._workspace_or(workspace), stream))
 
     def kv_read_quantised(self, kv_cache, block_table, q_start, q_len, ctx_len, k_rows, v_rows, num_pages: Optional[int] = None,
                           num_tokens: Optional[int] = None, stream=None):
         """``sarathi_kv_read_quantised``: what the cache holds of positions ctx_len - q_len .. ctx_len - 1, as rows."""
-        self._check_quantised(kv_cache, (k_rows, v_rows), num_tokens, q_len)
-        self._check(_marshal.kv_read_quantised(self._address(), self.config.max_blocks_per_seq, kv_cache, block_table, q_start, q_len,
+        self._check(_marshal.kv_read_quantised(self._address(), *self._widths, kv_cache, block_table, q_start, q_len,
                                                ctx_len, num_pages, num_tokens, k_rows, v_rows, stream))
         return k_rows, v_rows
 
     def hybrid_attention_quantised(self, q, kv_cache, block_table, q_start, q_len, ctx_len, sm_scale: float, out,
                                    num_pages: Optional[int] = None, num_tokens: Optional[int] = None, workspace=None, stream=None):
         """``sarathi_hybrid_attention_quantised``: ``hybrid_attention`` over the 4-bit cache."""
-        self._check_quantised(kv_cache)
-        self._check(_marshal.attention_quantised(self._address(), self.config.max_blocks_per_seq, q, kv_cache, block_table, q_start, q_len,
+        self._check(_marshal.attention_quantised(self._address(), *self._widths, q, kv_cache, block_table, q_start, q_len,
                                                  ctx_len, num_pages, num_tokens, float(sm_scale), out, stream, self._workspace_or(workspace)))
         return out
 
     def hybrid_attention_quantised_noalloc(self, q, kv_cache, block_table, q_start, q_len, ctx_len, sm_scale: float, out,
                                            num_pages: Optional[int] = None, num_tokens: Optional[int] = None, stream=None):
         """``sarathi_hybrid_attention_quantised_noalloc``: no workspace, the library's built-in scratch."""
-        self._check_quantised(kv_cache)
-        self._check(_marshal.attention_quantised(self._address(), self.config.max_blocks_per_seq, q, kv_cache, block_table, q_start, q_len,
+        self._check(_marshal.attention_quantised(self._address(), *self._widths, q, kv_cache, block_table, q_start, q_len,
                                                  ctx_len, num_pages, num_tokens, float(sm_scale), out, stream))
         return out
 

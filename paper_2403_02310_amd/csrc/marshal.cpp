@@ -36,7 +36,7 @@ NoallocQuantisedFn noalloc_quantised_fn;
 // registered by binding.py, kept for the life of the process
 PyObject *ndarray_type, *as_i32, *current_stream, *refuse_table;
 PyObject *as_c_int32, *as_c_int64, *as_c_address;
-PyObject *s_is_contiguous, *s_data_ptr, *s_shape, *s_cuda_stream;
+PyObject *s_is_contiguous, *s_data_ptr, *s_shape, *s_cuda_stream, *s_element_size;
 
 // An int as the C call takes it (wrapped to 64 bits), None and what is no int through `convert`, which takes and refuses what a
 // ctypes call does; sets an error otherwise.
@@ -236,13 +236,47 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return PyLong_FromLong(st);
 }
 
-// (handle, max_blocks, k_new, v_new, kv_cache, block_table, q_start, q_len, ctx_len, num_pages, num_tokens, workspace, stream)
+// What a pool of 4-bit records and the rows that go in and out of it must look like: the C call is given bare pointers.  The calls below
+// take (handle, max_blocks, KV heads, head_dim, bytes of a record, ...).
+struct Widths {
+    int64_t max_blocks, heads, dim, record;
+    bool get(PyObject *const *a) {
+        max_blocks = PyLong_AsLongLong(a[0]);
+        heads = PyLong_AsLongLong(a[1]);
+        dim = PyLong_AsLongLong(a[2]);
+        record = PyLong_AsLongLong(a[3]);
+        return !PyErr_Occurred();
+    }
+};
+// [first >= rows, second, third] of items of so many bytes; None and addresses pass
+bool tensor_fits(PyObject *t, const char *name, int64_t rows, int64_t second, int64_t third, int64_t item) {
+    if (t == Py_None || PyLong_Check(t)) return true;
+    PyObject *shape = PyObject_GetAttr(t, s_shape);
+    if (!shape) return false;
+    bool fits = PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 3 && PyLong_AsLongLong(PyTuple_GET_ITEM(shape, 0)) >= rows &&
+                PyLong_AsLongLong(PyTuple_GET_ITEM(shape, 1)) == second && PyLong_AsLongLong(PyTuple_GET_ITEM(shape, 2)) == third;
+    if (fits) {
+        PyObject *size = PyObject_CallMethodNoArgs(t, s_element_size);
+        fits = size && PyLong_AsLongLong(size) == item;
+        Py_XDECREF(size);
+    }
+    PyErr_Clear();
+    if (!fits) PyErr_Format(PyExc_ValueError, "%s must be [>= %lld, %lld, %lld] of %lld bytes each, got %S", name, (long long)rows, (long long)second,
+                            (long long)third, (long long)item, shape);
+    Py_DECREF(shape);
+    return fits;
+}
+bool pool_fits(PyObject *pool, const Widths &w) { return tensor_fits(pool, "kv_cache", 0, w.heads, w.record, 1); }
+
+// (..., k_new, v_new, kv_cache, block_table, q_start, q_len, ctx_len, num_pages, num_tokens, workspace, stream)
 PyObject *kv_append_quantised(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    if (!arity(n, 13)) return nullptr;
+    if (!arity(n, 16)) return nullptr;
     void *h, *k_new, *v_new, *cache, *ws, *stream;
+    Widths w;
     Batch b;
-    if (!device(a[0], &h) || !b.get(PyLong_AsLongLong(a[1]), a[5], a[6], a[7], a[8], a[9], a[10], a[4]) || !device(a[2], &k_new) ||
-        !device(a[3], &v_new) || !device(a[4], &cache) || !device(a[11], &ws) || !stream_of(a[12], &stream))
+    if (!device(a[0], &h) || !w.get(a + 1) || !pool_fits(a[7], w) || !b.get(w.max_blocks, a[8], a[9], a[10], a[11], a[12], a[13], a[7]) ||
+        !tensor_fits(a[5], "k_new", b.num_tokens, w.heads, w.dim, 2) || !tensor_fits(a[6], "v_new", b.num_tokens, w.heads, w.dim, 2) ||
+        !device(a[5], &k_new) || !device(a[6], &v_new) || !device(a[7], &cache) || !device(a[14], &ws) || !stream_of(a[15], &stream))
         return nullptr;
     int st;
     Py_BEGIN_ALLOW_THREADS
@@ -252,13 +286,15 @@ PyObject *kv_append_quantised(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return PyLong_FromLong(st);
 }
 
-// (handle, max_blocks, kv_cache, block_table, q_start, q_len, ctx_len, num_pages, num_tokens, k_rows, v_rows, stream)
+// (..., kv_cache, block_table, q_start, q_len, ctx_len, num_pages, num_tokens, k_rows, v_rows, stream)
 PyObject *kv_read_quantised(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    if (!arity(n, 12)) return nullptr;
+    if (!arity(n, 15)) return nullptr;
     void *h, *cache, *k_rows, *v_rows, *stream;
+    Widths w;
     Batch b;
-    if (!device(a[0], &h) || !b.get(PyLong_AsLongLong(a[1]), a[3], a[4], a[5], a[6], a[7], a[8], a[2]) || !device(a[2], &cache) ||
-        !device(a[9], &k_rows) || !device(a[10], &v_rows) || !stream_of(a[11], &stream))
+    if (!device(a[0], &h) || !w.get(a + 1) || !pool_fits(a[5], w) || !b.get(w.max_blocks, a[6], a[7], a[8], a[9], a[10], a[11], a[5]) ||
+        !tensor_fits(a[12], "k_rows", b.num_tokens, w.heads, w.dim, 2) || !tensor_fits(a[13], "v_rows", b.num_tokens, w.heads, w.dim, 2) ||
+        !device(a[5], &cache) || !device(a[12], &k_rows) || !device(a[13], &v_rows) || !stream_of(a[14], &stream))
         return nullptr;
     int st;
     Py_BEGIN_ALLOW_THREADS
@@ -268,20 +304,22 @@ PyObject *kv_read_quantised(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return PyLong_FromLong(st);
 }
 
-// (handle, max_blocks, q, kv_cache, block_table, q_start, q_len, ctx_len, num_pages, num_tokens, sm_scale, out, stream[, workspace]):
+// (..., q, kv_cache, block_table, q_start, q_len, ctx_len, num_pages, num_tokens, sm_scale, out, stream[, workspace]):
 // without a workspace the allocation-free call
 PyObject *attention_quantised(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    if (n != 13 && !arity(n, 14)) return nullptr;
+    if (n != 16 && !arity(n, 17)) return nullptr;
     void *h, *q, *cache, *out, *stream, *ws = nullptr;
+    Widths w;
     Batch b;
-    if (!device(a[0], &h) || !b.get(PyLong_AsLongLong(a[1]), a[4], a[5], a[6], a[7], a[8], a[9], a[3]) || !device(a[2], &q) || !device(a[3], &cache))
+    if (!device(a[0], &h) || !w.get(a + 1) || !pool_fits(a[6], w) || !b.get(w.max_blocks, a[7], a[8], a[9], a[10], a[11], a[12], a[6]) ||
+        !device(a[5], &q) || !device(a[6], &cache))
         return nullptr;
-    const float scale = static_cast<float>(PyFloat_AsDouble(a[10]));
-    if (PyErr_Occurred() || !device(a[11], &out) || !stream_of(a[12], &stream) || (n == 14 && !device(a[13], &ws))) return nullptr;
+    const float scale = static_cast<float>(PyFloat_AsDouble(a[13]));
+    if (PyErr_Occurred() || !device(a[14], &out) || !stream_of(a[15], &stream) || (n == 17 && !device(a[16], &ws))) return nullptr;
     const auto *table = static_cast<const int32_t *>(b.table);
     int st;
     Py_BEGIN_ALLOW_THREADS
-    if (n == 14)
+    if (n == 17)
         st = attention_quantised_fn(h, q, cache, table, b.q_start.data(), b.q_len.data(), b.ctx_len.data(), b.num_seqs, b.num_tokens, b.num_pages, scale, out, ws, stream);
     else
         st = noalloc_quantised_fn(h, q, cache, table, b.q_start.data(), b.q_len.data(), b.ctx_len.data(), b.num_seqs, b.num_tokens, b.num_pages, scale, out, stream);
@@ -355,6 +393,7 @@ PyMODINIT_FUNC PyInit__marshal() {
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_shape = PyUnicode_InternFromString("shape");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
-    if (!s_is_contiguous || !s_data_ptr || !s_shape || !s_cuda_stream) return nullptr;
+    s_element_size = PyUnicode_InternFromString("element_size");
+    if (!s_is_contiguous || !s_data_ptr || !s_shape || !s_cuda_stream || !s_element_size) return nullptr;
     return PyModule_Create(&module);
 }
