@@ -187,9 +187,10 @@ struct SoftmaxState {
 
 // The way out of a wave tile: the four wavefronts' results are merged in wavefront order through LDS (each publishes its own at
 // WS::kWaveElems times its number), and the block writes the final rows, or one set of partial rows if the tile is split across blocks.
+// col0: the first of the tile's columns that `st` holds sixteen of.
 template <int D, typename WS>
 __device__ __forceinline__ void wave_finish(const AttnParams &p, const TileDesc &it, int split, int kvh, int tid, uint16_t *smem,
-                                            const SoftmaxState<D> &st) {
+                                            const SoftmaxState<D> &st, int col0 = 0) {
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15;
@@ -214,13 +215,13 @@ __device__ __forceinline__ void wave_finish(const AttnParams &p, const TileDesc 
     __syncthreads();
     // Merge: thread t owns column t / 16 and D / 16 consecutive channels of it.
     constexpr int CH = D / 16;
-    const int mc = tid >> 4;
+    const int at = tid >> 4, mc = col0 + at;  // among these sixteen, and in the tile
     const int ch0 = (tid & 15) * CH;
     if (mc >= it.n_cols) return;
     float m_w[4], m_max = kNegSentinel;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-        m_w[w] = reinterpret_cast<const float *>(smem + w * WS::kWaveElems)[WS::kOutFloats + mc * 2];
+        m_w[w] = reinterpret_cast<const float *>(smem + w * WS::kWaveElems)[WS::kOutFloats + at * 2];
         m_max = fmaxf(m_max, m_w[w]);
     }
     float acc[CH];
@@ -231,8 +232,8 @@ __device__ __forceinline__ void wave_finish(const AttnParams &p, const TileDesc 
     for (int w = 0; w < 4; ++w) {
         const float wt = __builtin_amdgcn_exp2f(m_w[w] - m_max);
         const float *merge = reinterpret_cast<const float *>(smem + w * WS::kWaveElems);
-        l_tot += wt * merge[WS::kOutFloats + mc * 2 + 1];
-        const float *o_w = merge + mc * WS::kColStride + ch0;
+        l_tot += wt * merge[WS::kOutFloats + at * 2 + 1];
+        const float *o_w = merge + at * WS::kColStride + ch0;
 #pragma unroll
         for (int j = 0; j < CH; j += 4) {
             const f32x4 o4 = *reinterpret_cast<const f32x4 *>(o_w + j);

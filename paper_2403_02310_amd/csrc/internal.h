@@ -14,6 +14,7 @@ namespace sarathi {
 constexpr int kPageSize = 16;     // tokens per page (the only supported value)
 constexpr int kTileKeys = 32;     // keys per inner-loop tile = two pages = one MFMA contraction depth
 constexpr int kWaveCols = 16;     // query columns a wave tile carries (16x16x32 MFMA N dimension)
+constexpr int kQuantisedWaveCols = 32;  // over the 4-bit cache, whose codes are unpacked once for both halves
 constexpr int kTileCols = 128;    // query columns a chunk tile carries (4 waves x 32x32x16 MFMA N dimension)
 constexpr int kReduceCols = 8;    // columns one block of the merge kernel handles
 constexpr int kKindWave = 0;

@@ -142,7 +142,7 @@ void emit_units(Plan &plan, size_t first, size_t last, int64_t split_keys, int64
 // re-ordered in windows of that many sequence pieces, first the first column tile of each, then the second, and so on.
 // (29 heads per KV head, two KV heads of 64 channels: 512 decodes of 256-4096 keys 189 -> 167 us, 200 of 1024-8192 keys
 // 167 -> 137; 32 heads per KV head, two of 128 channels: 128 decodes 100 -> 87.)
-void pair_column_tiles(Plan &plan, size_t base, int32_t num_kv_heads, std::vector<uint32_t> &scratch) {
+void pair_column_tiles(Plan &plan, size_t base, int32_t num_kv_heads, int32_t wave_cols, std::vector<uint32_t> &scratch) {
     int64_t apart = 8;
     while (apart > 1 && (apart / 2) * num_kv_heads % 8 == 0) apart /= 2;
     if (apart == 1) return;  // neighbours meet anyway
@@ -175,7 +175,7 @@ void pair_column_tiles(Plan &plan, size_t base, int32_t num_kv_heads, std::vecto
     flush();
     for (uint32_t u : scratch) {  // pieces that the first column tile of their sequence does not have
         const TileDesc &t = tile_of(u);
-        const TileDesc &first = plan.tiles[(u & kTileMask) - (uint32_t)(t.col_begin / kWaveCols)];
+        const TileDesc &first = plan.tiles[(u & kTileMask) - (uint32_t)(t.col_begin / wave_cols)];
         if ((int32_t)(u >> kUnitTileBits) >= first.n_splits) plan.units[out++] = u;
     }
 }
@@ -592,9 +592,10 @@ void plan_attention(const sarathi_config &cfg, const Options &opt, const Workspa
     plan.shared_wave_keys = 0;
     plan.key_bytes = quantised ? (double)quantised_record_bytes(cfg.head_dim) / kPageSize : cfg.head_dim * 4.0;
     const int32_t G = cfg.num_q_heads / cfg.num_kv_heads;
-    int64_t min_cols = quantised ? INT64_MAX : opt.tile_min_cols;
-    if (min_cols <= 0) min_cols = chunks_as_wave_tiles(cfg, opt, ws, q_len, ctx_len, num_seqs) ? INT64_MAX : kChunkMinCols;
+    int64_t min_cols = opt.tile_min_cols;
+    if (min_cols <= 0) min_cols = !quantised && chunks_as_wave_tiles(cfg, opt, ws, q_len, ctx_len, num_seqs) ? INT64_MAX : kChunkMinCols;
 
+    const int32_t wave_cols = quantised ? kQuantisedWaveCols : kWaveCols;
     // Tiles: chunk tiles first, then wave tiles (two passes keep each kind contiguous).
     int64_t keys_of_kind[2] = {0, 0};
     size_t n_chunk_tiles = 0;
@@ -605,7 +606,7 @@ void plan_attention(const sarathi_config &cfg, const Options &opt, const Workspa
             const bool chunk = n_cols >= min_cols;   // prefill chunk: 128-column LDS-staged tiles
             if (chunk != (kind == kKindTile)) continue;
             const int32_t prefix = ctx_len[s] - q_len[s];
-            const int32_t width = chunk ? kTileCols : kWaveCols;
+            const int32_t width = chunk ? kTileCols : wave_cols;
             for (int64_t c0 = 0; c0 < n_cols; c0 += width) {
                 TileDesc t{};
                 t.seq = s;
@@ -622,7 +623,7 @@ void plan_attention(const sarathi_config &cfg, const Options &opt, const Workspa
                 t.ctx_len = ctx_len[s];
                 plan.tiles.push_back(t);
                 keys_of_kind[kind] += t.n_keys - t.key_lo;
-                if (!chunk && n_cols > kWaveCols) plan.shared_wave_keys += t.n_keys - t.key_lo;
+                if (!chunk && n_cols > wave_cols) plan.shared_wave_keys += t.n_keys - t.key_lo;
             }
         }
         if (pass == 0) n_chunk_tiles = plan.tiles.size();
@@ -782,7 +783,7 @@ void plan_attention(const sarathi_config &cfg, const Options &opt, const Workspa
         const int64_t n_units = (int64_t)(plan.units.size() - wave_base);
         plan.even_decode_pieces = 20 * (int64_t)plan.longest_wave_keys * n_units <= 27 * keys_of_kind[kKindWave];
     }
-    pair_column_tiles(plan, wave_base, cfg.num_kv_heads, scratch);
+    pair_column_tiles(plan, wave_base, cfg.num_kv_heads, wave_cols, scratch);
 }
 
 }  // namespace sarathi

@@ -43,10 +43,20 @@ __device__ __forceinline__ uint32_t pack_pair(uint32_t codes, uint32_t pair, flo
 }
 __device__ __forceinline__ float key_scale(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
 
+// The largest of the magnitudes of eight bf16 numbers, as the bits of a bf16 (infinity and NaN are the largest).
+__device__ __forceinline__ uint32_t largest_bits(const u32x4 &x) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = max(top, max(x[i] & 0x7FFFu, (x[i] >> 16) & 0x7FFFu));
+    return top;
+}
+constexpr uint32_t kInfBits = 0x7F80u;
+
 // ---------------------------------------------------------------------------------------
-// Wave tiles (decodes, tiny chunks): 16 query columns against a key range, a quarter of it to each wavefront, as in the bf16 cache's
-// path.  With the layout above a lane's share of an operand is one load of 16 bytes (8 with 64 channels), 1 KiB front to
-// back over the wavefront, straight into registers:
+// Attention.  A wavefront holds 16 or 32 query columns and goes over its keys 32 at a time.  Wave tiles (decodes, tiny chunks): 32 columns
+// against a key range, a quarter of it to each wavefront, as in the bf16 cache's path; a tile of up to 16 columns has code of
+// its own.  Chunk tiles: 128 columns, 32 to each wavefront.  With the layout above a lane's share of an operand is one load
+// of 16 bytes (8 with 64 channels), 1 KiB front to back over the wavefront, straight into registers:
 //   S^T[key, col]: A-row n of matrix instruction b is slot n of page b of the tile; contraction step s of lane group g is channels
 //                  (D/4) g + 8 s .. + 7, in the queries alike, so a lane's channels lie in one block and have one scale
 //   O^T[ch, col]:  accumulator lane (g, n) has the scores of slots 4 g .. + 3 of both pages, and the values of those eight are
@@ -60,169 +70,620 @@ struct QuantisedWaveSmem {
     static constexpr int kTotalElems = 4 * kWaveElems;
 };
 
-// A lane's share of a tile of 32 keys: codes, the bytes of its keys' scales, the scales of its values.
-template <int D>
-struct QuantisedTile {
-    typedef __attribute__((ext_vector_type(D / 32))) uint32_t codes;
-    codes k[2], v[2];
-    uint32_t k_scale[2];
-    f32x4 v_scale[2];
+// A lane's share of a tile of 32 keys: the codes of its keys and the bytes of their scales, the codes and the scales of its values.
+template <int WORDS>
+struct QuantisedKeys {
+    typedef __attribute__((ext_vector_type(WORDS))) uint32_t words;
+    words codes[2];
+    uint32_t scale[2];
+};
+template <int WORDS>
+struct QuantisedValues {
+    typedef __attribute__((ext_vector_type(WORDS))) uint32_t words;
+    words codes[2];
+};
+struct QuantisedScales {  // of the values
+    f32x4 of[2];
 };
 
-template <int D>
+// The two block-table entries of a tile, and the records they name: wave-uniform, by scalar loads and arithmetic.
+struct QuantisedPages {
+    int32_t entry[2];
+};
+typedef const __attribute__((address_space(1))) uint8_t *record_ptr;
+struct QuantisedRecords {
+    record_ptr of[2];
+};
+
 struct QuantisedLoads {
-    const uint8_t *head;   // page 0 of this KV head
+    record_ptr head;       // page 0 of this KV head
     const_i32_ptr bt;      // this sequence's block-table row
-    int64_t page_stride;   // bytes per page (all KV heads)
-    int64_t last_page_id;  // page ids are clamped: a corrupt table cannot fault
+    uint32_t page_stride;  // bytes per page (all KV heads)
+    int32_t last_page_id;  // page ids are clamped: a corrupt table cannot fault
     int32_t n_pages_seq;   // pages that hold positions < ctx_len; those behind are never dereferenced
-    uint32_t k_off, v_off, k_scale_off, v_scale_off;
-};
+    uint32_t k_off, v_off, k_scale_off, v_scale_off;  // this lane's, inside a record
 
-template <typename T, bool STREAM>
-__device__ __forceinline__ T load_as(const uint8_t *base, uint32_t off) {
-    const T *at = reinterpret_cast<const T *>(base + off);
-    if constexpr (STREAM) return __builtin_nontemporal_load(at);
-    else return *at;
-}
-
-template <int D, bool STREAM>
-__device__ __forceinline__ void load_tile(const QuantisedLoads<D> &ge, int tile, QuantisedTile<D> &t) {
-    using codes = typename QuantisedTile<D>::codes;
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        const int64_t entry = ge.bt[min(tile * 2 + b, ge.n_pages_seq - 1)];
-        const uint8_t *rec = ge.head + (entry < 0 ? 0 : (entry > ge.last_page_id ? ge.last_page_id : entry)) * ge.page_stride;
-        t.k[b] = load_as<codes, STREAM>(rec, ge.k_off);
-        t.v[b] = load_as<codes, STREAM>(rec, ge.v_off);
-        t.k_scale[b] = load_as<uint8_t, STREAM>(rec, ge.k_scale_off);
-        t.v_scale[b] = load_as<f32x4, STREAM>(rec, ge.v_scale_off);
+    template <int D>
+    __device__ __forceinline__ void init(const AttnParams &p, const TileDesc &it, int kvh) {
+        head = (record_ptr)p.k_cache + (int64_t)kvh * Record<D>::kBytes;
+        bt = (const_i32_ptr)(p.block_table + (int64_t)it.seq * p.max_blocks);
+        page_stride = (uint32_t)p.num_kv_heads * Record<D>::kBytes;
+        last_page_id = (int32_t)min(p.num_pages - 1, (int64_t)INT32_MAX);
+        n_pages_seq = (it.ctx_len + kPageSize - 1) / kPageSize;
     }
-}
-
-template <int D, bool STREAM, typename Claim>
-__device__ __forceinline__ int quantised_wave_path(const AttnParams &p, const TileDesc &it, int split, int kvh, uint16_t *smem, Claim claim) {
-    const int tid = thread_of_item();
-    const int lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n = lane & 15;
-    const int g = lane >> 4;
-    const int ctx = it.ctx_len;
-    const int prefix = ctx - it.q_len;
-    const int G = p.group;
-    UnitRange ur = unit_range(it, split);
-    {   // this wavefront's quarter of the unit (possibly empty: then it contributes weight zero)
-        const int quarter = ((ur.key_end - ur.key_begin + 3) / 4 + kTileKeys - 1) / kTileKeys * kTileKeys;
-        const int b = ur.key_begin + wave * quarter;   // a multiple of 32, as every piece start
-        ur.key_end = min(ur.key_end, b + quarter);
-        ur.key_begin = min(b, ur.key_end);
+    __device__ __forceinline__ QuantisedPages pages_of(int tile) const {
+        return QuantisedPages{{bt[min(tile * 2, n_pages_seq - 1)], bt[min(tile * 2 + 1, n_pages_seq - 1)]}};
     }
-    // Lanes beyond the tile's valid columns shadow column 0 of the tile and store nothing.
-    const int col = it.col_begin + (n < it.n_cols ? n : 0);
-    const int row = col / G;
-    const int head = kvh * G + (col - row * G);
-    const int pos_eff = min(prefix + row, ur.key_end - 1);                   // last key this column may see here
-    const int min_pos_eff = min(prefix + it.col_begin / G, ur.key_end - 1);  // the same for the tile's first column
-    // first key inside this column's sliding window, and the largest such key over the tile's columns
-    const int lo = p.window > 0 ? max(0, prefix + row - p.window + 1) : 0;
-    const int max_lo = p.window > 0 ? max(0, prefix + (it.col_begin + it.n_cols - 1) / G - p.window + 1) : 0;
-
-    bf16x8 qreg[D / 32];
-    {
-        const uint16_t *qp = p.q + ((int64_t)(it.q_start + row) * p.num_q_heads + head) * D + g * (D / 4);
+    __device__ __forceinline__ QuantisedRecords records(const QuantisedPages &pages) const {
+        QuantisedRecords r;
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s) qreg[s] = load_bf16x8(qp + s * 8);
+        for (int b = 0; b < 2; ++b) r.of[b] = head + (uint64_t)(uint32_t)min(max(pages.entry[b], 0), last_page_id) * page_stride;
+        return r;
     }
-    using R = Record<D>;
-    QuantisedLoads<D> ge;
-    ge.head = reinterpret_cast<const uint8_t *>(p.k_cache) + (int64_t)kvh * R::kBytes;
-    ge.bt = (const_i32_ptr)(p.block_table + (int64_t)it.seq * p.max_blocks);
-    ge.page_stride = (int64_t)p.num_kv_heads * R::kBytes;
-    ge.last_page_id = p.num_pages - 1;
-    ge.n_pages_seq = (ctx + kPageSize - 1) / kPageSize;
-    const int block = g * D / 128;  // of 32 channels: lane groups share one with 64
-    ge.k_off = (uint32_t)(block * 256 + n * 16 + (D == 64 ? (g & 1) * 8 : 0));
-    ge.v_off = (uint32_t)(R::kValues + lane * (D / 8));
-    ge.k_scale_off = (uint32_t)(R::kKeyScales + block * 16 + n);
-    ge.v_scale_off = (uint32_t)(R::kValueScales + g * 16);
-
-    SoftmaxState<D> st;
-#pragma unroll
-    for (int c = 0; c < D / 16; ++c) st.o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-    st.m = kNegSentinel;
-    st.l = 0.f;
-    const float scale = p.scale_log2;
-
-    auto process = [&](const QuantisedTile<D> &t, int tile) {
-        f32x4 s[2];
+    // Called once a tile: the lanes' offsets, seen as new, are added to the records by the loads themselves instead of being widened and
+    // added to `head` ahead of the loop, which takes a 64-bit addition per lane and load.
+    __device__ __forceinline__ void renew() { asm volatile("" : "+v"(k_off), "+v"(v_off), "+v"(k_scale_off), "+v"(v_scale_off)); }
+    template <typename T, bool STREAM>
+    static __device__ __forceinline__ T load_as(record_ptr base, uint32_t off) {
+        const auto *at = reinterpret_cast<const __attribute__((address_space(1))) T *>(base + off);
+        if constexpr (STREAM) return __builtin_nontemporal_load(at);
+        else return *at;
+    }
+    // What is loaded in one call stays together: results come back in order, and are waited for so.
+    template <bool STREAM, int WORDS>
+    __device__ __forceinline__ void load(const QuantisedRecords &r, QuantisedKeys<WORDS> &t) const {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            s[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-            const float ks = key_scale(t.k_scale[b]);
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i)
-                s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, unpack_word(t.k[b][i], ks)), qreg[i], s[b], 0, 0, 0);
+            t.scale[b] = load_as<uint8_t, STREAM>(r.of[b], k_scale_off);
+            t.codes[b] = load_as<typename QuantisedKeys<WORDS>::words, STREAM>(r.of[b], k_off);
         }
-        f32x4 vs[2] = {t.v_scale[0], t.v_scale[1]};
-        // Hidden keys: score -inf, and value scale 0, so that what a hidden slot holds (NaN among it) multiplies nothing.
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    template <bool STREAM, int WORDS>
+    __device__ __forceinline__ void load(const QuantisedRecords &r, QuantisedValues<WORDS> &t) const {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) t.codes[b] = load_as<typename QuantisedValues<WORDS>::words, STREAM>(r.of[b], v_off);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    template <bool STREAM>
+    __device__ __forceinline__ void load(const QuantisedRecords &r, QuantisedScales &t) const {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) t.of[b] = load_as<f32x4, STREAM>(r.of[b], v_scale_off);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+};
+
+// Queries of 16 columns as the second operand of the score instructions.
+//
+// Unpacked keys meet them as they are, in bf16.  Two column groups against the same keys take the keys packed instead
+// (v_mfma_scale_f32_16x16x128_f8f6f4: 4-bit keys with their scales, nothing to unpack), and a query is then two 8-bit numbers of four significant
+// bits, q = 2^e (h + l / 32) with 2^e 128 at most the column's largest: h is q rounded, l the rest, which has as many bits as l where q is more than 2^-15
+// of the column's largest, and is off by 2^-23 of that elsewhere.  Lane group g holds channels 16 g .. + 15 (and 64 + 16 g ..), where the instruction
+// has contraction indices 16 g .. and 64 + 16 g ..; with 64 channels the second half of the contraction takes the same keys again, and l.
+template <int D>
+struct PackedQueries {
+    typedef __attribute__((ext_vector_type(8))) int words;
+    static constexpr int kTerms = D / 64;  // instructions a page
+    words w[kTerms];
+    int scale[kTerms];
+
+    __device__ __forceinline__ void load(const uint16_t *row, int g) {
+        u32x4 x[D / 32];
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            x[i] = *reinterpret_cast<const u32x4 *>(row + 16 * g + (i / 2) * 64 + (i % 2) * 8);
+            top = max(top, largest_bits(x[i]));
+        }
+        top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+        const int e = max((int)(top >> 7) - 7, 5);  // the byte of 2^e: the largest is 128 to 256 units
+        const float unit = key_scale((uint32_t)(254 - e));
+        int h[2 * (D / 32)], l[2 * (D / 32)];
+#pragma unroll
+        for (int i = 0; i < 2 * (D / 32); ++i) {
+            h[i] = l[i] = 0;
+            pair<false>(x[i / 2][i % 2 * 2], unit, h[i], l[i]);
+            pair<true>(x[i / 2][i % 2 * 2 + 1], unit, h[i], l[i]);
+        }
+        const int byte = top < kInfBits ? e : 255;  // an infinite or NaN query: NaN scores
+        if constexpr (D == 128) {
+            w[0] = words{h[0], h[1], h[2], h[3], h[4], h[5], h[6], h[7]};
+            w[1] = words{l[0], l[1], l[2], l[3], l[4], l[5], l[6], l[7]};
+            scale[0] = byte;
+            scale[1] = byte == 255 ? 255 : byte - 5;
+        } else {
+            w[0] = words{h[0], h[1], h[2], h[3], l[0], l[1], l[2], l[3]};
+            scale[0] = byte == 255 || g < 2 ? byte : byte - 5;  // lane group g gives the scale of indices 32 g .. + 31
+        }
+    }
+    template <bool HIGH>
+    static __device__ __forceinline__ void pair(uint32_t bf16_pair, float unit, int &h, int &l) {
+        const float a = __builtin_bit_cast(float, bf16_pair << 16) * unit, b = __builtin_bit_cast(float, bf16_pair & 0xFFFF0000u) * unit;
+        h = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, h, HIGH);
+        const f32x2 back = __builtin_amdgcn_cvt_pk_f32_fp8(h, HIGH);
+        l = __builtin_amdgcn_cvt_pk_fp8_f32((a - back[0]) * 32.0f, (b - back[1]) * 32.0f, l, HIGH);
+    }
+    // Instruction TERM of a page's scores; 4: 4-bit keys, 0: 8-bit queries.
+    template <int TERM, typename Keys>
+    __device__ __forceinline__ f32x4 scores(const Keys &k, uint32_t k_scale, f32x4 s) const {
+        const words key = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(key, w[TERM], s, 4, 0, 0, (int)k_scale, 0, scale[TERM]);
+    }
+};
+
+// f(std::integral_constant<int, i>) for i = 0 .. N - 1
+template <int N, typename F>
+__device__ __forceinline__ void static_for(F f) {
+    if constexpr (N > 0) {
+        static_for<N - 1>(f);
+        f(std::integral_constant<int, N - 1>{});
+    }
+}
+
+// The largest of two score accumulators' numbers, NaN aside, without the instructions that fmaxf quietens its operands with.  The compiler
+// does not see that the assembly reads what matrix instructions write, and they need a distance: the median, which it does see and which
+// the others wait for, has it kept for both accumulators.
+__device__ __forceinline__ float largest_of(const f32x4 &a, const f32x4 &b) {
+    float top = __builtin_amdgcn_fmed3f(a[0], b[0], INFINITY);
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(top) : "v"(top), "v"(a[1]), "v"(a[2]));
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(top) : "v"(top), "v"(a[3]), "v"(b[1]));
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(top) : "v"(top), "v"(b[2]), "v"(b[3]));
+    return top;
+}
+
+// 16 NC columns of one wavefront against keys [key_begin, key_end): what a block's wavefronts share out, columns or keys.  Two loops go over
+// the keys: over_unpacked, whose loads run four tiles ahead of few instructions, where the records come from memory (wave tiles), and over_packed,
+// whose instructions run under one another, where they come out of a cache (chunk tiles).
+template <int D, int NC>
+struct QuantisedColumns {
+    static constexpr int kOperands = D / 16;  // of output instructions: 16 channels each
+    using Values = QuantisedValues<D / 32>;
+    SoftmaxState<D> st[NC];
+    float scale;
+    int pos_eff[NC], lo[NC];  // last key a column may see here, first key inside its sliding window
+    // of the wavefront's first column, and of its last one: tiles in between hide no key from any column (wave-uniform; a wavefront
+    // without columns of its own shadows the tile's first)
+    int min_pos_eff, max_lo;
+    f32x4 s[NC][2];  // a tile's scores, hidden keys at -inf
+    QuantisedLoads ge;
+
+    // col0: the first column, of the tile's first n_cols; lanes beyond them shadow the tile's first column and store nothing.
+    // query(column group, its row of q)
+    template <typename Query>
+    __device__ __forceinline__ void init(const AttnParams &p, const TileDesc &it, int kvh, int col0, int key_end, int lane, Query query) {
+        const int n = lane & 15, g = lane >> 4;
+        const int prefix = it.ctx_len - it.q_len;
+        const int G = p.group;
+        scale = p.scale_log2;
+#pragma unroll
+        for (int cg = 0; cg < NC; ++cg) {
+            const int mine = col0 + 16 * cg + n;
+            const int col = it.col_begin + (mine < it.n_cols ? mine : 0);
+            const int row = col / G;
+            const int head = kvh * G + (col - row * G);
+            pos_eff[cg] = min(prefix + row, key_end - 1);
+            lo[cg] = p.window > 0 ? max(0, prefix + row - p.window + 1) : 0;
+            query(cg, p.q + ((int64_t)(it.q_start + row) * p.num_q_heads + head) * D);
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) st[cg].o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+            st[cg].m = kNegSentinel;
+            st[cg].l = 0.f;
+        }
+        const int first = col0 < it.n_cols ? col0 : 0, last = col0 < it.n_cols ? min(col0 + 16 * NC, it.n_cols) - 1 : 0;
+        min_pos_eff = min(prefix + (it.col_begin + first) / G, key_end - 1);
+        max_lo = p.window > 0 ? max(0, prefix + (it.col_begin + last) / G - p.window + 1) : 0;
+        ge.template init<D>(p, it, kvh);
+        ge.v_off = (uint32_t)(Record<D>::kValues + lane * (D / 8));
+        ge.v_scale_off = (uint32_t)(Record<D>::kValueScales + g * 16);
+    }
+
+    // Hides what a column may not see.  of: the scales of the tile's values.
+    __device__ __forceinline__ void mask(f32x4 (&of)[2], int tile, int g) {
         if (tile * kTileKeys + (kTileKeys - 1) > min_pos_eff || tile * kTileKeys < max_lo) {  // wave-uniform: some lane must mask
+            // A hidden key's weight is 0, which a scale that is not finite (a NaN among the values, or what a slot behind the context
+            // holds) would turn into NaN.  Such a scale becomes 0, and the scores of those that see it NaN.
+            bool finite = true;
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int key = tile * kTileKeys + b * kPageSize + g * 4 + i;
-                    const bool seen = key <= pos_eff && key >= lo;
-                    s[b][i] = seen ? s[b][i] : -INFINITY;
-                    vs[b][i] = seen ? vs[b][i] : 0.f;
+                for (int i = 0; i < 4; ++i) finite &= __builtin_isfinite(of[b][i]);
+            if (!__all(finite)) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const bool bad = !__builtin_isfinite(of[b][i]);
+#pragma unroll
+                        for (int cg = 0; cg < NC; ++cg) s[cg][b][i] = bad ? __builtin_nanf("") : s[cg][b][i];
+                        of[b][i] = bad ? 0.f : of[b][i];
+                    }
+            }
+#pragma unroll
+            for (int cg = 0; cg < NC; ++cg)
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = tile * kTileKeys + b * kPageSize + g * 4 + i;
+                        s[cg][b][i] = (key <= pos_eff[cg] && key >= lo[cg]) ? s[cg][b][i] : -INFINITY;
+                    }
+        }
+    }
+    // A column's reference maximum, at least its largest score; what its numbers so far are multiplied by.  top: this lane's largest.
+    __device__ __forceinline__ float raise(int cg, float top) {
+        SoftmaxState<D> &x = st[cg];
+        float most = fmaxf(top, __shfl_xor(top, 16));
+        most = fmaxf(most, __shfl_xor(most, 32));
+        const float m_new = fmaxf(x.m, most * scale);
+        const float alpha = __builtin_amdgcn_exp2f(x.m - m_new);
+        x.l *= alpha;
+        x.m = m_new;
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) x.o[c] *= alpha;
+        return alpha;
+    }
+    // The first operand of output instructions C: channels 16 C .. + 15, the values of the eight slots that the lane's weights are of.
+    template <int C>
+    static __device__ __forceinline__ bf16x8 value_operand(const Values &t) {
+        const uint32_t a = t.codes[0][C / 2], b = t.codes[1][C / 2];
+        constexpr int first = C % 2 * 2;
+        return __builtin_bit_cast(bf16x8, u32x4{unpack_pair<first>(a, 1.f), unpack_pair<first + 1>(a, 1.f), unpack_pair<first>(b, 1.f),
+                                                unpack_pair<first + 1>(b, 1.f)});
+    }
+
+    template <bool STREAM, typename Claim>
+    __device__ __forceinline__ int over_unpacked(const AttnParams &p, const TileDesc &it, int kvh, int col0, int key_begin, int key_end, int lane, Claim claim) {
+        using Keys = QuantisedKeys<D / 32>;
+        constexpr int kAhead = NC == 1 ? 4 : 2;  // (what 256 registers hold)
+        const int n = lane & 15, g = lane >> 4;
+        bf16x8 q[NC][D / 32];
+        init(p, it, kvh, col0, key_end, lane, [&](int cg, const uint16_t *row) {
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) q[cg][i] = load_bf16x8(row + g * (D / 4) + i * 8);
+        });
+        const int block = D == 128 ? g : (g >> 1);  // the block of 32 channels of a lane's keys: with 64 channels two lane groups share one
+        ge.k_off = (uint32_t)(block * 256 + n * 16 + (D == 64 ? (g & 1) * 8 : 0));
+        ge.k_scale_off = (uint32_t)(Record<D>::kKeyScales + block * 16 + n);
+
+        struct Tile {
+            Keys k;
+            Values v;
+            QuantisedScales scales;
+        };
+        auto load = [&](const QuantisedPages &pages, Tile &t) {
+            const QuantisedRecords r = ge.records(pages);
+            ge.renew();
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                t.k.scale[b] = QuantisedLoads::load_as<uint8_t, STREAM>(r.of[b], ge.k_scale_off);
+                t.k.codes[b] = QuantisedLoads::load_as<typename Keys::words, STREAM>(r.of[b], ge.k_off);
+            }
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                t.scales.of[b] = QuantisedLoads::load_as<f32x4, STREAM>(r.of[b], ge.v_scale_off);
+                t.v.codes[b] = QuantisedLoads::load_as<typename Values::words, STREAM>(r.of[b], ge.v_off);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto process = [&](const Tile &t, int tile) {
+#pragma unroll
+            for (int cg = 0; cg < NC; ++cg) s[cg][0] = s[cg][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const bf16x8 k = __builtin_bit_cast(bf16x8, unpack_word(t.k.codes[b][i], key_scale(t.k.scale[b])));
+#pragma unroll
+                    for (int cg = 0; cg < NC; ++cg) s[cg][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[cg][i], s[cg][b], 0, 0, 0);
+                }
+            f32x4 of[2] = {t.scales.of[0], t.scales.of[1]};
+            mask(of, tile, g);
+            bf16x8 w[NC];
+            float top[NC];
+            bool higher = false;
+#pragma unroll
+            for (int cg = 0; cg < NC; ++cg) {
+                top[cg] = largest_of(s[cg][0], s[cg][1]);
+                higher |= top[cg] * scale > st[cg].m + kRescaleSlack;
+            }
+            // Only where a score exceeds the reference maximum by more than the slack is the column's maximum looked for across its lanes.
+            if (__any(higher)) {
+#pragma unroll
+                for (int cg = 0; cg < NC; ++cg) raise(cg, top[cg]);
+            }
+#pragma unroll
+            for (int cg = 0; cg < NC; ++cg) {
+                f32x8 x;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[cg][i / 4][i % 4], scale, -st[cg].m));
+                    st[cg].l += e;
+                    x[i] = e * of[i / 4][i % 4];
+                }
+                // rounded to bf16 for the matrix instruction: each weight is off by at most 2^-8 of itself, averaged down over the keys
+                w[cg] = __builtin_convertvector(x, bf16x8);
+            }
+            static_for<kOperands>([&](auto at) {
+                constexpr int c = decltype(at)::value;
+                const bf16x8 v = value_operand<c>(t.v);
+#pragma unroll
+                for (int cg = 0; cg < NC; ++cg) st[cg].o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[cg], st[cg].o[c], 0, 0, 0);
+            });
+        };
+
+        // kAhead tiles wait in registers, and the table entries of as many more: a tile's loads never wait for a scalar one.  The loop proper has no
+        // branch around a load, so that each wait is for as many loads as are younger than the tile's own.
+        int tile = key_begin / kTileKeys;
+        const int tile_end = key_begin >= key_end ? tile : (key_end + kTileKeys - 1) / kTileKeys;
+        if (tile >= tile_end) return claim();
+        Tile t[kAhead];
+        QuantisedPages pages[kAhead];
+        auto fetch = [&](QuantisedPages &to, int of_tile) {  // (beyond the range: the sequence's last page again, at most)
+            to = ge.pages_of(of_tile);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) fetch(pages[i], tile + i);
+        if (tile + 2 * kAhead <= tile_end) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                load(pages[i], t[i]);
+                fetch(pages[i], tile + kAhead + i);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (tile + i < tile_end) {
+                    load(pages[i], t[i]);
+                    fetch(pages[i], tile + kAhead + i);
                 }
         }
-        // The reference maximum is raised when a score exceeds it by more than the slack; only then is the column's maximum
-        // looked for across its four lanes.
-        float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))) * scale;
-        if (__any(top > st.m + kRescaleSlack)) {
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float m_new = fmaxf(st.m, top);
-            const float alpha = __builtin_amdgcn_exp2f(st.m - m_new);
-            st.l *= alpha;
-            st.m = m_new;
+        for (; tile + 2 * kAhead <= tile_end; tile += kAhead)
 #pragma unroll
-            for (int c = 0; c < D / 16; ++c) st.o[c] *= alpha;
+            for (int i = 0; i < kAhead; ++i) {
+                process(t[i], tile + i);
+                load(pages[i], t[i]);
+                fetch(pages[i], tile + 2 * kAhead + i);
+            }
+        const int claimed = claim();  // the next item's counter is read under the last loads
+        for (; tile < tile_end; tile += kAhead)
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (tile + i < tile_end) {
+                    process(t[i], tile + i);
+                    if (tile + kAhead + i < tile_end) load(pages[i], t[i]);
+                }
+        return claimed;
+    }
+
+    // A step forms the scores of the next tile, the weights of this one and the output of the one before.  None waits for another, so they are
+    // laid out in groups of matrix instructions and the vector arithmetic that runs under them; the scheduling barriers keep the
+    // groups, which the compiler would gather.
+    __device__ __forceinline__ void over_packed(const AttnParams &p, const TileDesc &it, int kvh, int col0, int key_begin, int key_end, int lane) {
+        using Keys = QuantisedKeys<4>;
+        constexpr int kAhead = 2;
+        static_assert(kOperands == 2 * NC * PackedQueries<D>::kTerms, "as many score instructions as output operands");
+        const int n = lane & 15, g = lane >> 4;
+        PackedQueries<D> packed[NC];
+        init(p, it, kvh, col0, key_end, lane, [&](int cg, const uint16_t *row) { packed[cg].load(row, g); });
+        const int block = D == 128 ? g : (g & 1);  // with 64 channels the upper two lane groups take the same keys as the lower two
+        ge.k_off = (uint32_t)(block * 256 + n * 16);
+        ge.k_scale_off = (uint32_t)(Record<D>::kKeyScales + block * 16 + n);
+
+        float top[NC];       // this lane's largest score
+        float raise_at[NC];  // the reference maximum is raised when one of them is larger
+        // Score instruction number SLOT of a tile: first of all pages and column groups, then the second ones that add to them.
+        auto score = [&](const Keys &t, f32x4 (&to)[NC][2], auto slot) {
+            constexpr int SLOT = decltype(slot)::value, TERM = SLOT / (2 * NC), b = SLOT / NC % 2, cg = SLOT % NC;
+            const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+            to[cg][b] = packed[cg].template scores<TERM>(t.codes[b], t.scale[b], TERM == 0 ? zero : to[cg][b]);
+        };
+        auto mask_and_top = [&](QuantisedScales &t, int tile) {
+            mask(t.of, tile, g);
+#pragma unroll
+            for (int cg = 0; cg < NC; ++cg) top[cg] = largest_of(s[cg][0], s[cg][1]);
+        };
+        uint32_t pT[NC][4];  // the previous tile's weights, as bf16: the second operands of its output instructions
+#pragma unroll
+        for (int cg = 0; cg < NC; ++cg)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pT[cg][i] = 0;
+        auto operand_of = [&](int cg) { return __builtin_bit_cast(bf16x8, u32x4{pT[cg][0], pT[cg][1], pT[cg][2], pT[cg][3]}); };
+        auto step = [&](const Values &before, const QuantisedScales &t, const Keys &next, QuantisedScales &next_scales, int tile, auto load_more) {
+            bool higher = false;
+#pragma unroll
+            for (int cg = 0; cg < NC; ++cg) higher |= top[cg] > raise_at[cg];
+            if (__any(higher)) {
+#pragma unroll
+                for (int cg = 0; cg < NC; ++cg) {
+                    const float alpha = raise(cg, top[cg]);
+                    raise_at[cg] = (st[cg].m + kRescaleSlack) / scale;
+                    const u32x4 w = __builtin_bit_cast(u32x4, __builtin_convertvector(__builtin_convertvector(operand_of(cg), f32x8) * alpha, bf16x8));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) pT[cg][i] = w[i];
+                }
+            }
+            f32x4 s_next[NC][2];
+            uint32_t p_new[NC][4];
+            float even = 0.f;
+            bf16x8 v = value_operand<0>(before);
+            bf16x8 p_old[NC];
+#pragma unroll
+            for (int cg = 0; cg < NC; ++cg) p_old[cg] = operand_of(cg);
+            auto weight = [&](int k) {
+                const int cg = k / 8, b = k / 4 % 2, i = k % 4;
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[cg][b][i], scale, -st[cg].m));
+                st[cg].l += e;
+                const float w = e * t.of[b][i];
+                // rounded to bf16 for the matrix instruction, as above
+                if (k & 1) {
+                    p_new[cg][k % 8 / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{even, w}, bf16x2));
+                    asm volatile("" : "+v"(p_new[cg][k % 8 / 2]), "+v"(st[cg].l));  // (they would be formed behind the next step's branch)
+                } else {
+                    even = w;
+                    asm volatile("" : "+v"(even), "+v"(st[cg].l));
+                }
+            };
+            __builtin_amdgcn_sched_barrier(0);
+            static_for<kOperands>([&](auto at) {
+                constexpr int c = decltype(at)::value;
+                score(next, s_next, at);
+#pragma unroll
+                for (int k = c * 8 * NC / kOperands; k < (c + 1) * 8 * NC / kOperands; ++k) weight(k);
+                __builtin_amdgcn_sched_barrier(0);
+                st[0].o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_old[0], st[0].o[c], 0, 0, 0);
+                bf16x8 v_next = v;
+                if constexpr (c + 1 < kOperands) v_next = value_operand<c + 1>(before);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int cg = 1; cg < NC; ++cg) st[cg].o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_old[cg], st[cg].o[c], 0, 0, 0);
+                v = v_next;
+            });
+            load_more();
+#pragma unroll
+            for (int cg = 0; cg < NC; ++cg) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b) s[cg][b] = s_next[cg][b];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) pT[cg][i] = p_new[cg][i];
+            }
+            mask_and_top(next_scales, tile + 1);
+        };
+
+        int tile = key_begin / kTileKeys;
+        const int tile_end = key_begin >= key_end ? tile : (key_end + kTileKeys - 1) / kTileKeys;
+        if (tile >= tile_end) return;
+        // Tile T lives in slot T - (first tile) modulo kAhead of three rings.  Its step takes the keys of T + 1, the values' scales of T and the values'
+        // codes of T - 1, and has those of kAhead tiles on loaded in their place; the table entries come a step before.  (Loads beyond the range:
+        // the sequence's last page again, at most.  The last step forms scores of whatever its neighbour's registers hold, which nothing reads.)
+        Keys keys[kAhead];
+        QuantisedScales scales[kAhead];
+        Values values[kAhead];
+        QuantisedPages entries[kAhead + 2];
+#pragma unroll
+        for (int i = 0; i < kAhead + 2; ++i) entries[i] = ge.pages_of(tile + i);
+        QuantisedPages entry = ge.pages_of(tile + kAhead + 2);
+        QuantisedRecords for_values = ge.records(entries[kAhead - 1]), for_scales = ge.records(entries[kAhead]), for_keys = ge.records(entries[kAhead + 1]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const QuantisedRecords r = ge.records(entries[i]);
+            ge.template load<false>(r, keys[i]);
+            ge.template load<false>(r, scales[i]);
+            if (i + 1 < kAhead) ge.template load<false>(r, values[i]);
         }
-        f32x8 w;
-        float psum = 0.f;
+        static_for<kOperands>([&](auto slot) { score(keys[0], s, slot); });
+        ge.template load<false>(for_scales, keys[0]);
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], scale, -st.m));
-                psum += e;
-                w[4 * b + i] = e * vs[b][i];
-            }
-        st.l += psum;
-        // rounded to bf16 for the matrix instruction: each weight is off by at most 2^-8 of itself, averaged down over the keys
-        const bf16x8 pT = __builtin_convertvector(w, bf16x8);
+            for (int j = 0; j < D / 32; ++j) values[kAhead - 1].codes[b][j] = 0;  // (the tile before the first)
 #pragma unroll
-        for (int c = 0; c < D / 16; c += 2) {
-            const uint32_t a = t.v[0][c / 2], b = t.v[1][c / 2];
-            const u32x4 even = {unpack_pair<0>(a, 1.f), unpack_pair<1>(a, 1.f), unpack_pair<0>(b, 1.f), unpack_pair<1>(b, 1.f)};
-            const u32x4 odd = {unpack_pair<2>(a, 1.f), unpack_pair<3>(a, 1.f), unpack_pair<2>(b, 1.f), unpack_pair<3>(b, 1.f)};
-            st.o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), pT, st.o[c], 0, 0, 0);
-            st.o[c + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), pT, st.o[c + 1], 0, 0, 0);
-        }
-    };
-
-    const int tile_begin = ur.key_begin / kTileKeys;
-    const int tile_end = ur.key_begin >= ur.key_end ? tile_begin : (ur.key_end + kTileKeys - 1) / kTileKeys;
-    int claimed = 0;
-    if (tid == 0) claimed = claim();
-    for (int tile = tile_begin; tile < tile_end; ++tile) {
-        QuantisedTile<D> t;
-        load_tile<D, STREAM>(ge, tile, t);
-        process(t, tile);
+        for (int cg = 0; cg < NC; ++cg) raise_at[cg] = kNegSentinel;
+        mask_and_top(scales[0], tile);
+        for (; tile + 2 * kAhead < tile_end; tile += kAhead)
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                constexpr int k = kAhead;
+                const QuantisedRecords later = ge.records(entry);
+                entry = ge.pages_of(tile + i + kAhead + 3);
+                __builtin_amdgcn_sched_barrier(0);
+                step(values[(i + k - 1) % k], scales[i], keys[(i + 1) % k], scales[(i + 1) % k], tile + i, [&] {
+                    ge.renew();
+                    ge.template load<false>(for_keys, keys[(i + 1) % k]);
+                    ge.template load<false>(for_scales, scales[i]);
+                    ge.template load<false>(for_values, values[(i + k - 1) % k]);
+                });
+                for_values = for_scales;
+                for_scales = for_keys;
+                for_keys = later;
+            }
+        for (; tile < tile_end; tile += kAhead)
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (tile + i < tile_end) {
+                    constexpr int k = kAhead;
+                    const QuantisedRecords later = ge.records(entry);
+                    entry = ge.pages_of(tile + i + kAhead + 3);
+                    step(values[(i + k - 1) % k], scales[i], keys[(i + 1) % k], scales[(i + 1) % k], tile + i, [&] {
+                        ge.renew();
+                        if (tile + i + k + 1 < tile_end) ge.template load<false>(for_keys, keys[(i + 1) % k]);
+                        if (tile + i + k < tile_end) ge.template load<false>(for_scales, scales[i]);
+                        if (tile + i + k - 1 < tile_end) ge.template load<false>(for_values, values[(i + k - 1) % k]);
+                    });
+                    for_values = for_scales;
+                    for_scales = for_keys;
+                    for_keys = later;
+                    if (tile + i + 1 == tile_end)
+                        static_for<kOperands>([&](auto at) {
+                            constexpr int c = decltype(at)::value;
+                            const bf16x8 v = value_operand<c>(values[i]);
+#pragma unroll
+                            for (int cg = 0; cg < NC; ++cg) st[cg].o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, operand_of(cg), st[cg].o[c], 0, 0, 0);
+                        });
+                }
     }
-    wave_finish<D, QuantisedWaveSmem<D>>(p, it, split, kvh, tid, smem, st);
+};
+
+// A wave tile: 16 or 32 columns, a quarter of the keys to each wavefront.
+template <int D, int NC, bool STREAM, typename Claim>
+__device__ __forceinline__ int quantised_wave_path(const AttnParams &p, const TileDesc &it, int split, int kvh, uint16_t *smem, Claim claim) {
+    const int tid = thread_of_item();
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const UnitRange ur = unit_range(it, split);
+    // this wavefront's quarter of the unit (possibly empty: then it contributes weight zero), which begins at a multiple of 32 as every piece does
+    const int quarter = ((ur.key_end - ur.key_begin + 3) / 4 + kTileKeys - 1) / kTileKeys * kTileKeys;
+    const int begin = min(ur.key_begin + wave * quarter, ur.key_end), end = min(begin + quarter, ur.key_end);
+    QuantisedColumns<D, NC> columns;
+    const int claimed = columns.template over_unpacked<STREAM>(p, it, kvh, 0, begin, end, tid & 63, [&] { return tid == 0 ? claim() : 0; });
+    wave_finish<D, QuantisedWaveSmem<D>>(p, it, split, kvh, tid, smem, columns.st[0]);
+    if constexpr (NC == 2) {
+        __syncthreads();
+        wave_finish<D, QuantisedWaveSmem<D>>(p, it, split, kvh, tid, smem, columns.st[1], 16);
+    }
     return claimed;
+}
+
+// A chunk tile: 128 columns, 32 to each wavefront, all of the unit's keys.  The four wavefronts read the same records at about the same
+// time, out of the compute unit's own cache but for the first; nothing is shared through LDS and no wavefront waits for another.
+template <int D>
+__device__ __forceinline__ void quantised_chunk_path(const AttnParams &p, const TileDesc &it, int split, int kvh) {
+    const int tid = thread_of_item();
+    const int lane = tid & 63, n = lane & 15, g = lane >> 4;
+    const int col0 = __builtin_amdgcn_readfirstlane(tid >> 6) * 32;
+    if (col0 >= it.n_cols) return;
+    const UnitRange ur = unit_range(it, split);
+    QuantisedColumns<D, 2> columns;
+    // the wavefront's last column sees no key behind its own, its first one none in front of its window
+    const int prefix = it.ctx_len - it.q_len, first_row = (it.col_begin + col0) / p.group, last_row = (it.col_begin + min(col0 + 32, it.n_cols) - 1) / p.group;
+    const int key_end = min(ur.key_end, prefix + last_row + 1);
+    const int key_begin = p.window > 0 ? max(ur.key_begin, (prefix + first_row - p.window + 1) / kTileKeys * kTileKeys) : ur.key_begin;
+    columns.over_packed(p, it, kvh, col0, key_begin, key_end, lane);
+#pragma unroll
+    for (int cg = 0; cg < 2; ++cg) {
+        const SoftmaxState<D> &x = columns.st[cg];
+        const int mine = col0 + 16 * cg + n;
+        float l = x.l + __shfl_xor(x.l, 16);
+        l += __shfl_xor(l, 32);
+        if (mine >= it.n_cols) continue;
+        if (ur.part_row < 0) {
+            const int col = it.col_begin + mine, row = col / p.group, head = kvh * p.group + (col - row * p.group);
+            uint16_t *op = p.out + ((int64_t)(it.q_start + row) * p.num_q_heads + head) * D + g * 4;
+            const float inv = 1.0f / l;
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) *reinterpret_cast<u32x2 *>(op + c * 16) = __builtin_bit_cast(u32x2, __builtin_convertvector(x.o[c] * inv, bf16x4));
+        } else {  // a piece's (reference maximum, sum, unnormalised output)
+            const int64_t prow = ((int64_t)(ur.part_row + mine) * p.num_kv_heads + kvh);
+            float *po = p.part_o + prow * D + g * 4;
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) *reinterpret_cast<f32x4 *>(po + c * 16) = x.o[c];
+            if (g == 0) {
+                p.part_ml[prow * 2 + 0] = x.m;
+                p.part_ml[prow * 2 + 1] = l;
+            }
+        }
+    }
 }
 
 template <int D>
@@ -231,9 +692,12 @@ struct QuantisedPaths {
     static constexpr int kWaveBlocksPerUnit = 2;
     template <bool STREAM, typename Claim>
     static __device__ __forceinline__ int wave(const AttnParams &p, const TileDesc &it, int split, int kvh, uint16_t *smem, Claim claim) {
-        return quantised_wave_path<D, STREAM>(p, it, split, kvh, smem, claim);
+        if (it.n_cols > 16) return quantised_wave_path<D, 2, STREAM>(p, it, split, kvh, smem, claim);
+        return quantised_wave_path<D, 1, STREAM>(p, it, split, kvh, smem, claim);
     }
-    static __device__ __forceinline__ void chunk(const AttnParams &, const TileDesc &, int, int, uint16_t *) {}
+    static __device__ __forceinline__ void chunk(const AttnParams &p, const TileDesc &it, int split, int kvh, uint16_t *) {
+        quantised_chunk_path<D>(p, it, split, kvh);
+    }
 };
 
 // ---------------------------------------------------------------------------------------
@@ -251,15 +715,6 @@ struct RowsThread {
     __device__ __forceinline__ int key_word() const { return (piece >> 2) * 256 + slot * 16 + (piece & 3) * 4; }
     __device__ __forceinline__ int key_scale() const { return Record<D>::kKeyScales + (piece >> 2) * 16 + slot; }
 };
-
-// The largest of the magnitudes of eight bf16 numbers, as the bits of a bf16 (infinity and NaN are the largest).
-__device__ __forceinline__ uint32_t largest_bits(const u32x4 &x) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) top = max(top, max(x[i] & 0x7FFFu, (x[i] >> 16) & 0x7FFFu));
-    return top;
-}
-constexpr uint32_t kInfBits = 0x7F80u;
 
 template <int D>
 __device__ __forceinline__ void kv_append_quantised_block(const AppendParams &p, const AppendUnit *units) {

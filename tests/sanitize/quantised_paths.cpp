@@ -1,7 +1,10 @@
 // The entry points of the 4-bit cache under AddressSanitizer / UndefinedBehaviorSanitizer, on the stand-ins of host_paths.cpp: the launchers
 // below walk the records and the plan as the kernels do, on heap blocks of exactly the documented sizes.
+#include "internal.h"
 #define main host_paths_main
+#define kWaveCols kQuantisedWaveCols
 #include "host_paths.cpp"
+#undef kWaveCols
 #undef main
 
 namespace sarathi {
