@@ -457,7 +457,13 @@ struct WaveCut {
 WaveCut cheapest_wave_cut(const sarathi_config &cfg, const Plan &plan, size_t n_chunk_tiles, int64_t wave_keys, int64_t tile_split, int64_t wave_split,
                           int64_t max_rows, bool chunks_made_do, bool plan_in_arguments) {
     const int64_t n_wave_tiles = (int64_t)(plan.tiles.size() - n_chunk_tiles);
-    const double key_us = cfg.head_dim * 4.0;  // bytes of a key and its value, one KV head
+    const double key_us = plan.key_bytes;  // of a key and its value, one KV head
+    // Over the 4-bit cache a block alone pulls 40 GB/s as well (320 keys a microsecond; with 64 channels 26 and 370), of fewer bytes, and the merge
+    // is cheap against it, so that cuts pay from 9 us by the estimate on (us a call, whole and cut: two decodes of up to 4725 keys, 16 and 2 heads,
+    // 21.8 and 12.0; 10 of up to 2270, 32 and 8 heads, 14.9 and 12.3; 3 of up to 1779, 56 and 8 heads, 13.0 and 11.0; 12 of up to 1202 11.6 and
+    // 12.8; 11 of up to 1541, 58 and 2 heads of 64 channels, 13.5 and 11.6).
+    const bool quantised = plan.key_bytes != cfg.head_dim * 4.0;
+    const double block_rate = quantised && cfg.head_dim == 64 ? 26.0e3 : 40.0e3, merge_us = quantised ? 2.5 : 5.3;
     double chunk_steps = 0.0;
     int64_t chunk_blocks = 0;
     bool chunk_cut = false;
@@ -495,7 +501,7 @@ WaveCut cheapest_wave_cut(const sarathi_config &cfg, const Plan &plan, size_t n_
                 most = std::max<int64_t>(most, ns);
             }
         }
-        const double block_us = (double)longest * key_us / 40.0e3;
+        const double block_us = (double)longest * key_us / block_rate;
         const double decode_us = 3.0 + std::max(stream_us, block_us) + 0.25 * std::min(stream_us, block_us) +
                                  2.0 * (double)((pieces * cfg.num_kv_heads - 1) / 512);
         if (rows > max_rows && most > 1) return 1.0e12;
@@ -505,7 +511,7 @@ WaveCut cheapest_wave_cut(const sarathi_config &cfg, const Plan &plan, size_t n_
         double c = std::max(decode_us, chunk_us) + 0.3 * std::min(decode_us, chunk_us);
         if (most > 1) {
             c += 0.25 * (double)most + 2.0 * (double)rows * cfg.num_kv_heads * (cfg.head_dim + 2) * 4.0 / 4.5e6;
-            if (!chunk_cut) c += 5.3;
+            if (!chunk_cut) c += merge_us;
         }
         return c;
     };
@@ -518,7 +524,8 @@ WaveCut cheapest_wave_cut(const sarathi_config &cfg, const Plan &plan, size_t n_
         }
     };
     const double host_us = (plan_in_arguments ? 15.8 : 12.8) + (plan_in_arguments ? 0.09 : 0.03) * (double)n_wave_tiles;
-    if (as_is >= 28.0 || (n_chunk_tiles == 0 && as_is >= 18.0 && host_us < (plan_in_arguments ? 0.8 : 0.85) * as_is)) {
+    const bool quantised_pays = quantised && !plan_in_arguments && n_chunk_tiles == 0 && as_is >= 9.0;
+    if (as_is >= 28.0 || quantised_pays || (n_chunk_tiles == 0 && as_is >= 18.0 && host_us < (plan_in_arguments ? 0.8 : 0.85) * as_is)) {
         if (whole > 0) search(whole);
         if (!best.few) search(0);
     }
@@ -576,6 +583,40 @@ bool chunks_as_wave_tiles(const sarathi_config &cfg, const Options &opt, const W
     return ws.meta_per_launch == 0 || attn_meta_bytes((size_t)tiles, (size_t)tiles, 0) <= ws.meta_per_launch;
 }
 
+// The same over the 4-bit cache, whose wave tiles of 32 columns reach 0.93 of the chunk tiles' rate where both fill the chip and come in four
+// times as many blocks.  They pay as long as those are few, and where the keys are not: a block's start and its four wavefronts' merge
+// want some work between them.  Next to decodes that stream for more than 0.3 of the time a chunk block takes, chunk tiles pay, which leave
+// them a slot on every compute unit, unless those are few and wait for a block longer than the chunk takes.  us a call, chunk tiles and wave tiles: 235 tokens behind 1258, 64 and 8 heads, 35.3 and 26.6; 580 behind 1774,
+// 58 and 2 heads of 64 channels, next to 6 decodes 50.4 and 39.4; 488 behind 3165 next to 186 of up to 777, 64 and 8 heads, 90.5 and 81.3; but
+// 272 behind 1 16.3 and 18.4, 1299 behind none and 749 behind 4211 145 and 156; 512 behind 1871 next to 64 of up to 4096, 32 and 8 heads, 56 and 71,
+// and 8 behind 410 next to 29 of up to 7659, 16 and 2 heads, 20.0 and 16.4.
+bool quantised_chunks_as_wave_tiles(const sarathi_config &cfg, const Options &opt, const WorkspaceLayout &ws, const int32_t *q_len,
+                                    const int32_t *ctx_len, int32_t num_seqs) {
+    if (opt.tile_split_keys > 0 || opt.resident_chunks == 1 || opt.interleave != 2) return false;  // asks for chunk tiles
+    const int64_t G = cfg.num_q_heads / cfg.num_kv_heads;
+    int64_t tiles = 0, chunk_tiles = 0, span = 0, other_span = 0, other_keys = 0;
+    for (int32_t s = 0; s < num_seqs; ++s) {
+        const int64_t n = ceil_div((int64_t)q_len[s] * G, kQuantisedWaveCols);
+        const int64_t keys = opt.window > 0 ? std::min<int64_t>(ctx_len[s], opt.window + q_len[s]) : ctx_len[s];
+        tiles += n;
+        if ((int64_t)q_len[s] * G < kChunkMinCols) {
+            other_keys += n * keys;
+            other_span = std::max(other_span, keys);
+        } else {
+            chunk_tiles += n;
+            span = std::max(span, keys);
+        }
+    }
+    if (chunk_tiles * cfg.num_kv_heads > (span < 1024 ? 512 : 1152)) return false;
+    const double chunk_us = (double)span / kTileKeys * (cfg.head_dim == 128 ? 0.57 : 0.4);
+    const double key_bytes = (double)quantised_record_bytes(cfg.head_dim) / kPageSize;
+    const double stream_us = (double)other_keys * cfg.num_kv_heads * key_bytes / 6.5e6;
+    const double other_us = (double)other_span * key_bytes / (cfg.head_dim == 128 ? 40.0e3 : 26.0e3);
+    if (stream_us > 0.3 * chunk_us && other_us < std::max(chunk_us, stream_us)) return false;
+    // a plan that travels in kernel arguments has to fit one launch so
+    return ws.meta_per_launch == 0 || attn_meta_bytes((size_t)tiles, (size_t)tiles, 0) <= ws.meta_per_launch;
+}
+
 }  // namespace
 
 void plan_attention(const sarathi_config &cfg, const Options &opt, const WorkspaceLayout &ws,
@@ -593,7 +634,11 @@ void plan_attention(const sarathi_config &cfg, const Options &opt, const Workspa
     plan.key_bytes = quantised ? (double)quantised_record_bytes(cfg.head_dim) / kPageSize : cfg.head_dim * 4.0;
     const int32_t G = cfg.num_q_heads / cfg.num_kv_heads;
     int64_t min_cols = opt.tile_min_cols;
-    if (min_cols <= 0) min_cols = !quantised && chunks_as_wave_tiles(cfg, opt, ws, q_len, ctx_len, num_seqs) ? INT64_MAX : kChunkMinCols;
+    if (min_cols <= 0) {
+        const bool as_wave_tiles = quantised ? quantised_chunks_as_wave_tiles(cfg, opt, ws, q_len, ctx_len, num_seqs)
+                                             : chunks_as_wave_tiles(cfg, opt, ws, q_len, ctx_len, num_seqs);
+        min_cols = as_wave_tiles ? INT64_MAX : kChunkMinCols;
+    }
 
     const int32_t wave_cols = quantised ? kQuantisedWaveCols : kWaveCols;
     // Tiles: chunk tiles first, then wave tiles (two passes keep each kind contiguous).
@@ -642,8 +687,8 @@ void plan_attention(const sarathi_config &cfg, const Options &opt, const Workspa
     // needs up to 0.4 of that time (a block streams about 25 GB/s next to a second one on its compute unit) is
     // dealt out first and is done well before the launch ends, and every cut avoided saves partial rows and,
     // for a batch without other cuts, the merge launch.
-    const double wave_stream_us = (double)keys_of_kind[kKindWave] * cfg.num_kv_heads * cfg.head_dim * 4.0 / 5.0e6;
-    const int64_t wave_floor = std::max<int64_t>(4 * kMinWaveKeys, (int64_t)(0.4 * wave_stream_us * 25000.0 / (cfg.head_dim * 4.0)));
+    const double wave_stream_us = (double)keys_of_kind[kKindWave] * cfg.num_kv_heads * plan.key_bytes / 5.0e6;
+    const int64_t wave_floor = std::max<int64_t>(4 * kMinWaveKeys, (int64_t)(0.4 * wave_stream_us * 25000.0 / plan.key_bytes));
     int64_t wave_split = pick(4 * opt.split_keys, keys_of_kind[kKindWave], std::max<int64_t>(1, opt.target_items / 4), wave_floor);
     // Chunk tiles: enough units per KV head to put two blocks on every compute unit (a block
     // alone on its unit cannot hide its per-step latencies), but never pieces below the floor.
@@ -686,7 +731,7 @@ void plan_attention(const sarathi_config &cfg, const Options &opt, const Workspa
     // heads, 44.7 and 52.4 us.  Were 10 % to be promised, 6 would be, and the average 0.879 x.)  Forced roles and separate
     // launches get the same cuts: 90 batches with such options are on average within 2 % with and without them.
     auto cheaper_next_to_decodes = [&](int64_t keys, int64_t max_rows) {
-        const double key_us = cfg.head_dim * 4.0;
+        const double key_us = plan.key_bytes;
         const int64_t wave_block_keys = std::min(longest_wave_span, wave_split + wave_split / 2);
         HybridBatch b{(double)keys_of_kind[kKindWave] * cfg.num_kv_heads * key_us / 6.5e6, (double)wave_block_keys * key_us / 68.0e3,
                       (int64_t)(plan.tiles.size() - n_chunk_tiles) * cfg.num_kv_heads, 2 * plan.shared_wave_keys > keys_of_kind[kKindWave]};
