@@ -125,6 +125,25 @@ def test_read_back_of_arbitrary_records(hx, shape, q_len, ctx):
         np.testing.assert_array_equal(qref._f64(got[n:]), 7.0)
 
 
+@pytest.mark.parametrize("shape", sorted(SHAPES))
+def test_read_back_of_many_pages(hx, shape):
+    """More pages than a launch's arguments hold, one, two and an odd number of KV heads, ragged ends: rows bit for bit."""
+    s = SHAPES[shape]
+    b = wl._make("read_many", s, [1500, 1, 1777, 33, 250], [1507, 40, 1777, 35, 999], 46)
+    h = hx.make_handle(b)
+    pool = np.full(h.quantised_cache_shape(b.num_pages), 0x21, np.uint8)
+    d, rng = s.head_dim, np.random.default_rng(47)
+    pool[..., :16 * d] = rng.integers(0, 256, pool[..., :16 * d].shape)
+    pool[..., 16 * d:16 * d + d // 2] = rng.integers(120, 135, pool[..., 16 * d:16 * d + d // 2].shape)
+    pool[..., 16 * d + d // 2:] = np.full(pool.shape[:2] + (16,), 0.6875, np.float32).view(np.uint8)
+    k, v = (torch.full((b.num_tokens + 3, s.num_kv_heads, d), 7.0, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    h.kv_read_quantised(torch.from_numpy(pool).cuda(), torch.from_numpy(b.block_table).cuda(), b.q_start, b.q_len, b.ctx_len, k, v)
+    for got, ref in zip((k, v), qref.read(pool, b.block_table, b.q_len, b.ctx_len, d)):
+        got = hx.device_to_bits(got)
+        np.testing.assert_array_equal(qref._f64(got[:b.num_tokens]), qref._f64(ref))
+        np.testing.assert_array_equal(qref._f64(got[b.num_tokens:]), 7.0)
+
+
 def _rows_bits(values):
     return wl.f32_to_bf16_bits(np.asarray(values, np.float32))
 
