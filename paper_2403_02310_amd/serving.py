@@ -3,7 +3,7 @@
 Each iteration builds a batch (stall-free batching, Algorithm 3 of section 4.2, through
 ``sarathi_build_stall_free_batch``), grows the paged KV cache of the scheduled sequences,
 appends their new K/V rows and runs hybrid-batch attention (``sarathi_kv_append``,
-``sarathi_hybrid_attention``).  Only attention runs (there is no model around it), so iteration
+``sarathi_hybrid_attention``, or their forms over the 4-bit cache).  Only attention runs (there is no model around it), so iteration
 times are a PROXY for the paper's time-between-tokens: they show how the cost of an iteration
 varies with what the scheduler put into it, not end-to-end latency.
 
@@ -134,13 +134,18 @@ class GpuBackend:
     """Device memory (torch) + the two device entry points.  Fails loudly if the library is missing."""
 
     def __init__(self, seed: int = 0, keep_outputs: bool = True, options: Optional[Dict[str, int]] = None,
-                 linear_model: Optional[str] = None):
-        """``linear_model`` (a key of ``linear_layers.MODELS``): every iteration also runs the four linear layers of
+                 linear_model: Optional[str] = None, cache: str = "bf16"):
+        """``cache``: "bf16", or "4bit" for keys and values held in 4 bits (0.27 of the bytes).
+
+        ``linear_model`` (a key of ``linear_layers.MODELS``): every iteration also runs the four linear layers of
         one transformer layer of that model over the iteration's tokens (random weights, outputs unused), so that the
         timed iteration holds the operators that dominate a real one (section 3.1), not attention alone."""
+        if cache not in ("bf16", "4bit"):
+            raise ValueError("unknown cache %r" % cache)
         import torch
         from . import binding
         self.torch, self.binding = torch, binding
+        self.cache = cache
         self.seed, self.keep_outputs, self.options = seed, keep_outputs, dict(options or {})
         self.linear_model = linear_model
         self.linear = []
@@ -152,13 +157,17 @@ class GpuBackend:
         draw = lambda heads: torch.randn(total, heads, s.head_dim, device="cuda", generator=g).to(torch.bfloat16)
         self.q_all, self.k_all, self.v_all = draw(s.num_q_heads), draw(s.num_kv_heads), draw(s.num_kv_heads)
         self.out_all = torch.zeros_like(self.q_all) if self.keep_outputs else None
-        self.k_cache = torch.zeros(loop.pool.num_pages, s.num_kv_heads, s.page_size, s.head_dim, device="cuda", dtype=torch.bfloat16)
-        self.v_cache = torch.zeros(loop.pool.num_pages, s.num_kv_heads, s.head_dim, s.page_size, device="cuda", dtype=torch.bfloat16)
         self.bt_all = torch.full((loop.max_seqs, loop.max_blocks), -1, device="cuda", dtype=torch.int32)
+        self.max_tokens = loop.max_tokens
         self.handle = self.binding.Handle(s.num_q_heads, s.num_kv_heads, s.head_dim, max_tokens=loop.max_tokens,
                                           max_seqs=loop.max_seqs, max_blocks_per_seq=loop.max_blocks)
         for k, v in self.options.items():
             self.handle.set_option(k, v)
+        if self.cache == "4bit":
+            self.kv_cache = torch.zeros(self.handle.quantised_cache_shape(loop.pool.num_pages), device="cuda", dtype=torch.uint8)
+        else:
+            self.k_cache = torch.zeros(loop.pool.num_pages, s.num_kv_heads, s.page_size, s.head_dim, device="cuda", dtype=torch.bfloat16)
+            self.v_cache = torch.zeros(loop.pool.num_pages, s.num_kv_heads, s.head_dim, s.page_size, device="cuda", dtype=torch.bfloat16)
         self.sm_scale = 1.0 / float(np.sqrt(s.head_dim))
         self._ev = (torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True))
         if self.linear_model:
@@ -177,6 +186,22 @@ class GpuBackend:
         t = self.torch.tensor(list(pages), dtype=self.torch.int32)
         self.bt_all[slot, first_block:first_block + len(pages)] = t.cuda()
 
+    def cached_rows(self, request: Request):
+        """Keys and values of a running request's positions, as the 4-bit cache holds them (bf16 rows): what leaves with a request that
+        another cache takes over."""
+        if self.cache != "4bit":
+            raise ValueError("the bf16 cache holds the rows that were appended")
+        n = request.num_prefilled + request.num_decoded
+        if not request.pages or n == 0:
+            raise ValueError("request %d holds no pages" % request.id)
+        rows = [self.torch.empty((n,) + tuple(self.k_all.shape[1:]), device="cuda", dtype=self.torch.bfloat16) for _ in range(2)]
+        bt, start = self.bt_all[request.slot:request.slot + 1], np.zeros(1, np.int32)
+        for at in range(0, n, self.max_tokens):   # as many rows as the handle takes in a call
+            end = min(n, at + self.max_tokens)
+            self.handle.kv_read_quantised(self.kv_cache, bt, start, np.array([end - at], np.int32), np.array([end], np.int32),
+                                          *(x[at:end] for x in rows))
+        return rows
+
     def run(self, loop: "ServingLoop", slots, token_rows, q_start, q_len, ctx_len) -> float:
         torch = self.torch
         rows = torch.from_numpy(np.asarray(token_rows, dtype=np.int64)).cuda()
@@ -185,8 +210,12 @@ class GpuBackend:
         out = torch.empty_like(q)
         q_start, q_len, ctx_len = (np.asarray(a, dtype=np.int32) for a in (q_start, q_len, ctx_len))
         self._ev[0].record()
-        self.handle.kv_append(k_new, v_new, self.k_cache, self.v_cache, bt, q_start, q_len, ctx_len)
-        self.handle.hybrid_attention(q, self.k_cache, self.v_cache, bt, q_start, q_len, ctx_len, self.sm_scale, out)
+        if self.cache == "4bit":
+            self.handle.kv_append_quantised(k_new, v_new, self.kv_cache, bt, q_start, q_len, ctx_len)
+            self.handle.hybrid_attention_quantised(q, self.kv_cache, bt, q_start, q_len, ctx_len, self.sm_scale, out)
+        else:
+            self.handle.kv_append(k_new, v_new, self.k_cache, self.v_cache, bt, q_start, q_len, ctx_len)
+            self.handle.hybrid_attention(q, self.k_cache, self.v_cache, bt, q_start, q_len, ctx_len, self.sm_scale, out)
         n_tok = int(q.shape[0])
         for x, w, y in self.linear:   # a smaller workspace than a token count would like only means fewer pieces
             self.binding.linear(x[:n_tok], w, y[:n_tok], self.linear_scratch)

@@ -62,12 +62,15 @@ def compute_token_budget(rows: Sequence[Dict[str, float]], target_seconds: float
 
 
 def gpu_timer(options: Optional[Dict[str, int]] = None, reps: int = 20, warmup: int = 3,
-              linear_model: Optional[str] = None, on_batch: Optional[Callable] = None) -> Callable[[HybridBatch], float]:
+              linear_model: Optional[str] = None, on_batch: Optional[Callable] = None, cache: str = "bf16") -> Callable[[HybridBatch], float]:
     """Times append + attention of a batch on the GPU (median of ``reps``), values drawn on the device.
     ``linear_model`` (a key of ``linear_layers.MODELS``): the four linear layers of one transformer layer of that
     model run over the batch's tokens inside the timed region too.  ``on_batch(batch, tensors)`` is called after
     a batch has been timed with its device tensors (q, k_cache, v_cache, block_table, out), e.g. by a test that
-    checks what the profiled launches computed."""
+    checks what the profiled launches computed.  ``cache``: "bf16", or "4bit" for keys and values held in 4 bits
+    (the tensors are then q, kv_cache, block_table, out; the cache is filled by appends)."""
+    if cache not in ("bf16", "4bit"):
+        raise ValueError("unknown cache %r" % cache)
     import torch
     from . import binding
     linear = []   # (weight, scratch bytes wanted) per layer, drawn once
@@ -94,18 +97,30 @@ def gpu_timer(options: Optional[Dict[str, int]] = None, reps: int = 20, warmup: 
             h.set_option(k, v)
         g = torch.Generator(device="cuda").manual_seed(b.seed)
         rnd = lambda *shape: torch.randn(*shape, device="cuda", generator=g).to(torch.bfloat16)
-        kc = rnd(b.num_pages, s.num_kv_heads, s.page_size, s.head_dim)
-        vc = rnd(b.num_pages, s.num_kv_heads, s.head_dim, s.page_size)
+        if cache == "bf16":
+            kc = rnd(b.num_pages, s.num_kv_heads, s.page_size, s.head_dim)
+            vc = rnd(b.num_pages, s.num_kv_heads, s.head_dim, s.page_size)
         q, kn, vn = rnd(b.num_tokens, s.num_q_heads, s.head_dim), rnd(b.num_tokens, s.num_kv_heads, s.head_dim), rnd(b.num_tokens, s.num_kv_heads, s.head_dim)
         out = torch.empty_like(q)
         bt = torch.from_numpy(b.block_table).cuda()
+        if cache == "4bit":
+            kv = torch.zeros(h.quantised_cache_shape(b.num_pages), device="cuda", dtype=torch.uint8)
+            for i in range(b.num_seqs):   # every position once, in pieces that the handle takes
+                for at in range(0, int(b.ctx_len[i]), 2048):
+                    n = np.array([min(2048, int(b.ctx_len[i]) - at)], np.int32)
+                    rows = rnd(2, int(n[0]), s.num_kv_heads, s.head_dim)
+                    h.kv_append_quantised(rows[0], rows[1], kv, bt[i:i + 1], np.zeros(1, np.int32), n, n + np.int32(at))
         ev = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
         lin_ops = linear_operands(b.num_tokens) if linear_model else []
         times = []
         for i in range(warmup + reps):
             ev[0].record()
-            h.kv_append(kn, vn, kc, vc, bt, b.q_start, b.q_len, b.ctx_len)
-            h.hybrid_attention(q, kc, vc, bt, b.q_start, b.q_len, b.ctx_len, b.sm_scale, out)
+            if cache == "4bit":
+                h.kv_append_quantised(kn, vn, kv, bt, b.q_start, b.q_len, b.ctx_len)
+                h.hybrid_attention_quantised(q, kv, bt, b.q_start, b.q_len, b.ctx_len, b.sm_scale, out)
+            else:
+                h.kv_append(kn, vn, kc, vc, bt, b.q_start, b.q_len, b.ctx_len)
+                h.hybrid_attention(q, kc, vc, bt, b.q_start, b.q_len, b.ctx_len, b.sm_scale, out)
             for x, w, y, scratch in lin_ops:
                 binding.linear(x, w, y, scratch)
             ev[1].record()
@@ -113,7 +128,8 @@ def gpu_timer(options: Optional[Dict[str, int]] = None, reps: int = 20, warmup: 
             if i >= warmup:
                 times.append(ev[0].elapsed_time(ev[1]) * 1e-3)
         if on_batch is not None:
-            on_batch(b, {"q": q, "k_cache": kc, "v_cache": vc, "block_table": bt, "out": out})
+            held = {"kv_cache": kv} if cache == "4bit" else {"k_cache": kc, "v_cache": vc}
+            on_batch(b, {"q": q, **held, "block_table": bt, "out": out})
         return float(np.median(times))
     return time_batch
 

@@ -121,3 +121,13 @@ def test_host_paths_are_clean_under_asan_and_ubsan(tmp_path):
     assert res.returncode == 0, res.stdout[-2000:] + res.stderr[-6000:]
     assert "quantised paths clean" in res.stdout
     assert "ERROR: AddressSanitizer" not in res.stderr and "runtime error" not in res.stderr, res.stderr[-6000:]
+
+
+def test_unknown_caches_are_refused_before_anything_else():
+    from paper_2403_02310_amd import serving, token_budget
+    with pytest.raises(ValueError):
+        serving.GpuBackend(cache="8bit")
+    with pytest.raises(ValueError):
+        token_budget.gpu_timer(cache="8bit")
+    with pytest.raises(ValueError):
+        serving.GpuBackend().cached_rows(None)
