@@ -56,9 +56,8 @@ constexpr uint32_t kInfBits = 0x7F80u;
 // Attention.  A wavefront holds 16 or 32 query columns and goes over its keys 32 at a time.  Wave tiles (decodes, tiny chunks): 32 columns
 // against a key range, a quarter of it to each wavefront, as in the bf16 cache's path; a tile of up to 16 columns has code of
 // its own.  Chunk tiles: 128 columns, 32 to each wavefront.  With the layout above a lane's share of an operand is one load
-// of 16 bytes (8 with 64 channels), 1 KiB front to back over the wavefront, straight into registers:
-//   S^T[key, col]: A-row n of matrix instruction b is slot n of page b of the tile; contraction step s of lane group g is channels
-//                  (D/4) g + 8 s .. + 7, in the queries alike, so a lane's channels lie in one block and have one scale
+// of 16 bytes (of values with 64 channels 8), front to back over the wavefront, straight into registers:
+//   S^T[key, col]: A-row n of matrix instruction b is slot n of page b of the tile, lane group g the channels of block g and its scale
 //   O^T[ch, col]:  accumulator lane (g, n) has the scores of slots 4 g .. + 3 of both pages, and the values of those eight are
 //                  the contraction indices of its lane group
 // ---------------------------------------------------------------------------------------
@@ -71,10 +70,8 @@ struct QuantisedWaveSmem {
 };
 
 // A lane's share of a tile of 32 keys: the codes of its keys and the bytes of their scales, the codes and the scales of its values.
-template <int WORDS>
 struct QuantisedKeys {
-    typedef __attribute__((ext_vector_type(WORDS))) uint32_t words;
-    words codes[2];
+    u32x4 codes[2];
     uint32_t scale[2];
 };
 template <int WORDS>
@@ -130,12 +127,12 @@ struct QuantisedLoads {
         else return *at;
     }
     // What is loaded in one call stays together: results come back in order, and are waited for so.
-    template <bool STREAM, int WORDS>
-    __device__ __forceinline__ void load(const QuantisedRecords &r, QuantisedKeys<WORDS> &t) const {
+    template <bool STREAM>
+    __device__ __forceinline__ void load(const QuantisedRecords &r, QuantisedKeys &t) const {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             t.scale[b] = load_as<uint8_t, STREAM>(r.of[b], k_scale_off);
-            t.codes[b] = load_as<typename QuantisedKeys<WORDS>::words, STREAM>(r.of[b], k_off);
+            t.codes[b] = load_as<u32x4, STREAM>(r.of[b], k_off);
         }
         __builtin_amdgcn_sched_barrier(0);
     }
@@ -153,13 +150,13 @@ struct QuantisedLoads {
     }
 };
 
-// Queries of 16 columns as the second operand of the score instructions.
-//
-// Unpacked keys meet them as they are, in bf16.  Two column groups against the same keys take the keys packed instead
-// (v_mfma_scale_f32_16x16x128_f8f6f4: 4-bit keys with their scales, nothing to unpack), and a query is then two 8-bit numbers of four significant
-// bits, q = 2^e (h + l / 32) with 2^e 128 at most the column's largest: h is q rounded, l the rest, which has as many bits as l where q is more than 2^-15
-// of the column's largest, and is off by 2^-23 of that elsewhere.  Lane group g holds channels 16 g .. + 15 (and 64 + 16 g ..), where the instruction
-// has contraction indices 16 g .. and 64 + 16 g ..; with 64 channels the second half of the contraction takes the same keys again, and l.
+// Queries of 16 columns as the second operand of the score instructions, v_mfma_scale_f32_16x16x128_f8f6f4: the first takes 4-bit keys with their
+// scales as they are held, nothing to unpack (against keys unpacked to bf16, four instructions and 32 conversions for two: 512 tokens
+// next to 64 decodes of 32 and 8 heads 56.6 us and 52.9, 200 decodes of 58 and 2 heads of 64 channels 44.4 and 41.2).  The second takes 8-bit numbers of four
+// significant bits, so a query is two of them, q = 2^e (h + l / 32) with 2^e 128 at most the column's largest: h is q rounded, l the rest.  That is q
+// itself where it is more than 2^-15 of the column's largest, and off by at most 2^-23 of that elsewhere, as a sum in 32 bits that holds the
+// largest is.  Lane group g holds channels 16 g .. + 15 (and 64 + 16 g ..), where the instruction has contraction indices 16 g .. and 64 + 16 g ..;
+// with 64 channels the second half of the contraction takes the same keys again, and l.
 template <int D>
 struct PackedQueries {
     typedef __attribute__((ext_vector_type(8))) int words;
@@ -205,8 +202,8 @@ struct PackedQueries {
         l = __builtin_amdgcn_cvt_pk_fp8_f32((a - back[0]) * 32.0f, (b - back[1]) * 32.0f, l, HIGH);
     }
     // Instruction TERM of a page's scores; 4: 4-bit keys, 0: 8-bit queries.
-    template <int TERM, typename Keys>
-    __device__ __forceinline__ f32x4 scores(const Keys &k, uint32_t k_scale, f32x4 s) const {
+    template <int TERM>
+    __device__ __forceinline__ f32x4 scores(const u32x4 &k, uint32_t k_scale, f32x4 s) const {
         const words key = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
         return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(key, w[TERM], s, 4, 0, 0, (int)k_scale, 0, scale[TERM]);
     }
@@ -233,13 +230,16 @@ __device__ __forceinline__ float largest_of(const f32x4 &a, const f32x4 &b) {
 }
 
 // 16 NC columns of one wavefront against keys [key_begin, key_end): what a block's wavefronts share out, columns or keys.  Two loops go over
-// the keys: over_unpacked, whose loads run four tiles ahead of few instructions, where the records come from memory (wave tiles), and over_packed,
-// whose instructions run under one another, where they come out of a cache (chunk tiles).
+// the keys.  over_streamed, where the records come from memory (wave tiles): two or four tiles of loads in flight, few instructions; 256 decodes of 32 and 8
+// heads read 418 MB in 71 us, 5.9 TB/s, 512 of 64 and 8 heads 1334 MB in 214, 6.2 TB/s, which is the bound.  over_cached, where they come out of
+// a cache (chunk tiles): the issue of vector and matrix instructions is the bound, which run under one another here; 2048 tokens of 64 and 8
+// heads take 144 us, 0.97 Pflop/s, and 166 through the other loop.
 template <int D, int NC>
 struct QuantisedColumns {
     static constexpr int kOperands = D / 16;  // of output instructions: 16 channels each
     using Values = QuantisedValues<D / 32>;
     SoftmaxState<D> st[NC];
+    PackedQueries<D> packed[NC];
     float scale;
     int pos_eff[NC], lo[NC];  // last key a column may see here, first key inside its sliding window
     // of the wavefront's first column, and of its last one: tiles in between hide no key from any column (wave-uniform; a wavefront
@@ -249,9 +249,7 @@ struct QuantisedColumns {
     QuantisedLoads ge;
 
     // col0: the first column, of the tile's first n_cols; lanes beyond them shadow the tile's first column and store nothing.
-    // query(column group, its row of q)
-    template <typename Query>
-    __device__ __forceinline__ void init(const AttnParams &p, const TileDesc &it, int kvh, int col0, int key_end, int lane, Query query) {
+    __device__ __forceinline__ void init(const AttnParams &p, const TileDesc &it, int kvh, int col0, int key_end, int lane) {
         const int n = lane & 15, g = lane >> 4;
         const int prefix = it.ctx_len - it.q_len;
         const int G = p.group;
@@ -264,7 +262,7 @@ struct QuantisedColumns {
             const int head = kvh * G + (col - row * G);
             pos_eff[cg] = min(prefix + row, key_end - 1);
             lo[cg] = p.window > 0 ? max(0, prefix + row - p.window + 1) : 0;
-            query(cg, p.q + ((int64_t)(it.q_start + row) * p.num_q_heads + head) * D);
+            packed[cg].load(p.q + ((int64_t)(it.q_start + row) * p.num_q_heads + head) * D, g);
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) st[cg].o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
             st[cg].m = kNegSentinel;
@@ -274,6 +272,9 @@ struct QuantisedColumns {
         min_pos_eff = min(prefix + (it.col_begin + first) / G, key_end - 1);
         max_lo = p.window > 0 ? max(0, prefix + (it.col_begin + last) / G - p.window + 1) : 0;
         ge.template init<D>(p, it, kvh);
+        const int block = D == 128 ? g : (g & 1);  // of 32 channels; with 64 channels the upper two lane groups take the same keys as the lower two
+        ge.k_off = (uint32_t)(block * 256 + n * 16);
+        ge.k_scale_off = (uint32_t)(Record<D>::kKeyScales + block * 16 + n);
         ge.v_off = (uint32_t)(Record<D>::kValues + lane * (D / 8));
         ge.v_scale_off = (uint32_t)(Record<D>::kValueScales + g * 16);
     }
@@ -333,21 +334,13 @@ struct QuantisedColumns {
     }
 
     template <bool STREAM, typename Claim>
-    __device__ __forceinline__ int over_unpacked(const AttnParams &p, const TileDesc &it, int kvh, int col0, int key_begin, int key_end, int lane, Claim claim) {
-        using Keys = QuantisedKeys<D / 32>;
+    __device__ __forceinline__ int over_streamed(const AttnParams &p, const TileDesc &it, int kvh, int col0, int key_begin, int key_end, int lane, Claim claim) {
         constexpr int kAhead = NC == 1 ? 4 : 2;  // (what 256 registers hold)
-        const int n = lane & 15, g = lane >> 4;
-        bf16x8 q[NC][D / 32];
-        init(p, it, kvh, col0, key_end, lane, [&](int cg, const uint16_t *row) {
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) q[cg][i] = load_bf16x8(row + g * (D / 4) + i * 8);
-        });
-        const int block = D == 128 ? g : (g >> 1);  // the block of 32 channels of a lane's keys: with 64 channels two lane groups share one
-        ge.k_off = (uint32_t)(block * 256 + n * 16 + (D == 64 ? (g & 1) * 8 : 0));
-        ge.k_scale_off = (uint32_t)(Record<D>::kKeyScales + block * 16 + n);
+        const int g = lane >> 4;
+        init(p, it, kvh, col0, key_end, lane);
 
         struct Tile {
-            Keys k;
+            QuantisedKeys k;
             Values v;
             QuantisedScales scales;
         };
@@ -357,7 +350,7 @@ struct QuantisedColumns {
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 t.k.scale[b] = QuantisedLoads::load_as<uint8_t, STREAM>(r.of[b], ge.k_scale_off);
-                t.k.codes[b] = QuantisedLoads::load_as<typename Keys::words, STREAM>(r.of[b], ge.k_off);
+                t.k.codes[b] = QuantisedLoads::load_as<u32x4, STREAM>(r.of[b], ge.k_off);
             }
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
@@ -369,14 +362,13 @@ struct QuantisedColumns {
         auto process = [&](const Tile &t, int tile) {
 #pragma unroll
             for (int cg = 0; cg < NC; ++cg) s[cg][0] = s[cg][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+            static_for<PackedQueries<D>::kTerms>([&](auto term) {
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i)
+                for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const bf16x8 k = __builtin_bit_cast(bf16x8, unpack_word(t.k.codes[b][i], key_scale(t.k.scale[b])));
-#pragma unroll
-                    for (int cg = 0; cg < NC; ++cg) s[cg][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[cg][i], s[cg][b], 0, 0, 0);
-                }
+                    for (int cg = 0; cg < NC; ++cg)
+                        s[cg][b] = packed[cg].template scores<decltype(term)::value>(t.k.codes[b], t.k.scale[b], s[cg][b]);
+            });
             f32x4 of[2] = {t.scales.of[0], t.scales.of[1]};
             mask(of, tile, g);
             bf16x8 w[NC];
@@ -460,21 +452,16 @@ struct QuantisedColumns {
     // A step forms the scores of the next tile, the weights of this one and the output of the one before.  None waits for another, so they are
     // laid out in groups of matrix instructions and the vector arithmetic that runs under them; the scheduling barriers keep the
     // groups, which the compiler would gather.
-    __device__ __forceinline__ void over_packed(const AttnParams &p, const TileDesc &it, int kvh, int col0, int key_begin, int key_end, int lane) {
-        using Keys = QuantisedKeys<4>;
+    __device__ __forceinline__ void over_cached(const AttnParams &p, const TileDesc &it, int kvh, int col0, int key_begin, int key_end, int lane) {
         constexpr int kAhead = 2;
         static_assert(kOperands == 2 * NC * PackedQueries<D>::kTerms, "as many score instructions as output operands");
-        const int n = lane & 15, g = lane >> 4;
-        PackedQueries<D> packed[NC];
-        init(p, it, kvh, col0, key_end, lane, [&](int cg, const uint16_t *row) { packed[cg].load(row, g); });
-        const int block = D == 128 ? g : (g & 1);  // with 64 channels the upper two lane groups take the same keys as the lower two
-        ge.k_off = (uint32_t)(block * 256 + n * 16);
-        ge.k_scale_off = (uint32_t)(Record<D>::kKeyScales + block * 16 + n);
+        const int g = lane >> 4;
+        init(p, it, kvh, col0, key_end, lane);
 
         float top[NC];       // this lane's largest score
         float raise_at[NC];  // the reference maximum is raised when one of them is larger
         // Score instruction number SLOT of a tile: first of all pages and column groups, then the second ones that add to them.
-        auto score = [&](const Keys &t, f32x4 (&to)[NC][2], auto slot) {
+        auto score = [&](const QuantisedKeys &t, f32x4 (&to)[NC][2], auto slot) {
             constexpr int SLOT = decltype(slot)::value, TERM = SLOT / (2 * NC), b = SLOT / NC % 2, cg = SLOT % NC;
             const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
             to[cg][b] = packed[cg].template scores<TERM>(t.codes[b], t.scale[b], TERM == 0 ? zero : to[cg][b]);
@@ -490,7 +477,7 @@ struct QuantisedColumns {
 #pragma unroll
             for (int i = 0; i < 4; ++i) pT[cg][i] = 0;
         auto operand_of = [&](int cg) { return __builtin_bit_cast(bf16x8, u32x4{pT[cg][0], pT[cg][1], pT[cg][2], pT[cg][3]}); };
-        auto step = [&](const Values &before, const QuantisedScales &t, const Keys &next, QuantisedScales &next_scales, int tile, auto load_more) {
+        auto step = [&](const Values &before, const QuantisedScales &t, const QuantisedKeys &next, QuantisedScales &next_scales, int tile, auto load_more) {
             bool higher = false;
 #pragma unroll
             for (int cg = 0; cg < NC; ++cg) higher |= top[cg] > raise_at[cg];
@@ -557,7 +544,7 @@ struct QuantisedColumns {
         // Tile T lives in slot T - (first tile) modulo kAhead of three rings.  Its step takes the keys of T + 1, the values' scales of T and the values'
         // codes of T - 1, and has those of kAhead tiles on loaded in their place; the table entries come a step before.  (Loads beyond the range:
         // the sequence's last page again, at most.  The last step forms scores of whatever its neighbour's registers hold, which nothing reads.)
-        Keys keys[kAhead];
+        QuantisedKeys keys[kAhead];
         QuantisedScales scales[kAhead];
         Values values[kAhead];
         QuantisedPages entries[kAhead + 2];
@@ -636,7 +623,7 @@ __device__ __forceinline__ int quantised_wave_path(const AttnParams &p, const Ti
     const int quarter = ((ur.key_end - ur.key_begin + 3) / 4 + kTileKeys - 1) / kTileKeys * kTileKeys;
     const int begin = min(ur.key_begin + wave * quarter, ur.key_end), end = min(begin + quarter, ur.key_end);
     QuantisedColumns<D, NC> columns;
-    const int claimed = columns.template over_unpacked<STREAM>(p, it, kvh, 0, begin, end, tid & 63, [&] { return tid == 0 ? claim() : 0; });
+    const int claimed = columns.template over_streamed<STREAM>(p, it, kvh, 0, begin, end, tid & 63, [&] { return tid == 0 ? claim() : 0; });
     wave_finish<D, QuantisedWaveSmem<D>>(p, it, split, kvh, tid, smem, columns.st[0]);
     if constexpr (NC == 2) {
         __syncthreads();
@@ -659,7 +646,7 @@ __device__ __forceinline__ void quantised_chunk_path(const AttnParams &p, const 
     const int prefix = it.ctx_len - it.q_len, first_row = (it.col_begin + col0) / p.group, last_row = (it.col_begin + min(col0 + 32, it.n_cols) - 1) / p.group;
     const int key_end = min(ur.key_end, prefix + last_row + 1);
     const int key_begin = p.window > 0 ? max(ur.key_begin, (prefix + first_row - p.window + 1) / kTileKeys * kTileKeys) : ur.key_begin;
-    columns.over_packed(p, it, kvh, col0, key_begin, key_end, lane);
+    columns.over_cached(p, it, kvh, col0, key_begin, key_end, lane);
 #pragma unroll
     for (int cg = 0; cg < 2; ++cg) {
         const SoftmaxState<D> &x = columns.st[cg];
