@@ -70,17 +70,13 @@ struct QuantisedWaveSmem {
 };
 
 // A lane's share of a tile of 32 keys: the codes of its keys and the bytes of their scales, the codes and the scales of its values.
-struct QuantisedKeys {
-    u32x4 codes[2];
-    uint32_t scale[2];
-};
-template <int WORDS>
-struct QuantisedValues {
-    typedef __attribute__((ext_vector_type(WORDS))) uint32_t words;
-    words codes[2];
-};
-struct QuantisedScales {  // of the values
-    f32x4 of[2];
+template <int D>
+struct QuantisedTile {
+    typedef __attribute__((ext_vector_type(D / 32))) uint32_t words;
+    u32x4 keys[2];
+    uint32_t key_scales[2];
+    words values[2];
+    f32x4 value_scales[2];
 };
 
 // The two block-table entries of a tile, and the records they name: wave-uniform, by scalar loads and arithmetic.
@@ -126,26 +122,21 @@ struct QuantisedLoads {
         if constexpr (STREAM) return __builtin_nontemporal_load(at);
         else return *at;
     }
-    // What is loaded in one call stays together: results come back in order, and are waited for so.
-    template <bool STREAM>
-    __device__ __forceinline__ void load(const QuantisedRecords &r, QuantisedKeys &t) const {
+    // Loads of one tile stay together: results come back in order, and are waited for so.
+    template <bool STREAM, int D>
+    __device__ __forceinline__ void load(const QuantisedPages &pages, QuantisedTile<D> &t) {
+        const QuantisedRecords r = records(pages);
+        renew();
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            t.scale[b] = load_as<uint8_t, STREAM>(r.of[b], k_scale_off);
-            t.codes[b] = load_as<u32x4, STREAM>(r.of[b], k_off);
+            t.key_scales[b] = load_as<uint8_t, STREAM>(r.of[b], k_scale_off);
+            t.keys[b] = load_as<u32x4, STREAM>(r.of[b], k_off);
         }
-        __builtin_amdgcn_sched_barrier(0);
-    }
-    template <bool STREAM, int WORDS>
-    __device__ __forceinline__ void load(const QuantisedRecords &r, QuantisedValues<WORDS> &t) const {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) t.codes[b] = load_as<typename QuantisedValues<WORDS>::words, STREAM>(r.of[b], v_off);
-        __builtin_amdgcn_sched_barrier(0);
-    }
-    template <bool STREAM>
-    __device__ __forceinline__ void load(const QuantisedRecords &r, QuantisedScales &t) const {
-#pragma unroll
-        for (int b = 0; b < 2; ++b) t.of[b] = load_as<f32x4, STREAM>(r.of[b], v_scale_off);
+        for (int b = 0; b < 2; ++b) {
+            t.value_scales[b] = load_as<f32x4, STREAM>(r.of[b], v_scale_off);
+            t.values[b] = load_as<typename QuantisedTile<D>::words, STREAM>(r.of[b], v_off);
+        }
         __builtin_amdgcn_sched_barrier(0);
     }
 };
@@ -229,15 +220,17 @@ __device__ __forceinline__ float largest_of(const f32x4 &a, const f32x4 &b) {
     return top;
 }
 
-// 16 NC columns of one wavefront against keys [key_begin, key_end): what a block's wavefronts share out, columns or keys.  Two loops go over
-// the keys.  over_streamed, where the records come from memory (wave tiles): two or four tiles of loads in flight, few instructions; 256 decodes of 32 and 8
-// heads read 418 MB in 71 us, 5.9 TB/s, 512 of 64 and 8 heads 1334 MB in 214, 6.2 TB/s, which is the bound.  over_cached, where they come out of
-// a cache (chunk tiles): the issue of vector and matrix instructions is the bound, which run under one another here; 2048 tokens of 64 and 8
-// heads take 144 us, 0.97 Pflop/s, and 166 through the other loop.
+// 16 NC columns of one wavefront against keys [key_begin, key_end): what a block's wavefronts share out, columns or keys.
+//
+// kAhead tiles wait in registers.  Where the records come from memory (wave tiles) that is four, or two with 32 columns (us a call with one: 200 decodes
+// of 58 and 2 heads of 64 channels 41 and 54; with two instead of four: 64 decodes of 32 and 8 heads next to 512 tokens 52.6 and 55.3), and the memory is the
+// bound: 256 decodes of 32 and 8 heads read 418 MB in 71 us, 5.9 TB/s, 512 of 64 and 8 heads 1334 MB in 214, 6.2 TB/s.  Where they come out of a cache
+// (chunk tiles) it is one, and issue is the bound, of vector and matrix instructions, which the two wavefronts of a SIMD run under each other: 2048
+// tokens of 64 and 8 heads take 142 us, 0.99 Pflop/s (with two tiles 145; three wavefronts do not fit the registers).
 template <int D, int NC>
 struct QuantisedColumns {
     static constexpr int kOperands = D / 16;  // of output instructions: 16 channels each
-    using Values = QuantisedValues<D / 32>;
+    using Tile = QuantisedTile<D>;
     SoftmaxState<D> st[NC];
     PackedQueries<D> packed[NC];
     float scale;
@@ -311,8 +304,8 @@ struct QuantisedColumns {
                     }
         }
     }
-    // A column's reference maximum, at least its largest score; what its numbers so far are multiplied by.  top: this lane's largest.
-    __device__ __forceinline__ float raise(int cg, float top) {
+    // A column's reference maximum becomes at least its largest score.  top: this lane's.
+    __device__ __forceinline__ void raise(int cg, float top) {
         SoftmaxState<D> &x = st[cg];
         float most = fmaxf(top, __shfl_xor(top, 16));
         most = fmaxf(most, __shfl_xor(most, 32));
@@ -322,43 +315,21 @@ struct QuantisedColumns {
         x.m = m_new;
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) x.o[c] *= alpha;
-        return alpha;
     }
     // The first operand of output instructions C: channels 16 C .. + 15, the values of the eight slots that the lane's weights are of.
     template <int C>
-    static __device__ __forceinline__ bf16x8 value_operand(const Values &t) {
-        const uint32_t a = t.codes[0][C / 2], b = t.codes[1][C / 2];
+    static __device__ __forceinline__ bf16x8 value_operand(const Tile &t) {
+        const uint32_t a = t.values[0][C / 2], b = t.values[1][C / 2];
         constexpr int first = C % 2 * 2;
         return __builtin_bit_cast(bf16x8, u32x4{unpack_pair<first>(a, 1.f), unpack_pair<first + 1>(a, 1.f), unpack_pair<first>(b, 1.f),
                                                 unpack_pair<first + 1>(b, 1.f)});
     }
 
-    template <bool STREAM, typename Claim>
-    __device__ __forceinline__ int over_streamed(const AttnParams &p, const TileDesc &it, int kvh, int col0, int key_begin, int key_end, int lane, Claim claim) {
-        constexpr int kAhead = NC == 1 ? 4 : 2;  // (what 256 registers hold)
+    template <bool STREAM, int kAhead, typename Claim>
+    __device__ __forceinline__ int run(const AttnParams &p, const TileDesc &it, int kvh, int col0, int key_begin, int key_end, int lane, Claim claim) {
         const int g = lane >> 4;
         init(p, it, kvh, col0, key_end, lane);
 
-        struct Tile {
-            QuantisedKeys k;
-            Values v;
-            QuantisedScales scales;
-        };
-        auto load = [&](const QuantisedPages &pages, Tile &t) {
-            const QuantisedRecords r = ge.records(pages);
-            ge.renew();
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                t.k.scale[b] = QuantisedLoads::load_as<uint8_t, STREAM>(r.of[b], ge.k_scale_off);
-                t.k.codes[b] = QuantisedLoads::load_as<u32x4, STREAM>(r.of[b], ge.k_off);
-            }
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                t.scales.of[b] = QuantisedLoads::load_as<f32x4, STREAM>(r.of[b], ge.v_scale_off);
-                t.v.codes[b] = QuantisedLoads::load_as<typename Values::words, STREAM>(r.of[b], ge.v_off);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        };
         auto process = [&](const Tile &t, int tile) {
 #pragma unroll
             for (int cg = 0; cg < NC; ++cg) s[cg][0] = s[cg][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -367,9 +338,9 @@ struct QuantisedColumns {
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                     for (int cg = 0; cg < NC; ++cg)
-                        s[cg][b] = packed[cg].template scores<decltype(term)::value>(t.k.codes[b], t.k.scale[b], s[cg][b]);
+                        s[cg][b] = packed[cg].template scores<decltype(term)::value>(t.keys[b], t.key_scales[b], s[cg][b]);
             });
-            f32x4 of[2] = {t.scales.of[0], t.scales.of[1]};
+            f32x4 of[2] = {t.value_scales[0], t.value_scales[1]};
             mask(of, tile, g);
             bf16x8 w[NC];
             float top[NC];
@@ -398,13 +369,13 @@ struct QuantisedColumns {
             }
             static_for<kOperands>([&](auto at) {
                 constexpr int c = decltype(at)::value;
-                const bf16x8 v = value_operand<c>(t.v);
+                const bf16x8 v = value_operand<c>(t);
 #pragma unroll
                 for (int cg = 0; cg < NC; ++cg) st[cg].o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[cg], st[cg].o[c], 0, 0, 0);
             });
         };
 
-        // kAhead tiles wait in registers, and the table entries of as many more: a tile's loads never wait for a scalar one.  The loop proper has no
+        // The table entries of as many more tiles wait as well: a tile's loads never wait for a scalar one.  The loop proper has no
         // branch around a load, so that each wait is for as many loads as are younger than the tile's own.
         int tile = key_begin / kTileKeys;
         const int tile_end = key_begin >= key_end ? tile : (key_end + kTileKeys - 1) / kTileKeys;
@@ -420,14 +391,14 @@ struct QuantisedColumns {
         if (tile + 2 * kAhead <= tile_end) {
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                load(pages[i], t[i]);
+                ge.template load<STREAM>(pages[i], t[i]);
                 fetch(pages[i], tile + kAhead + i);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < kAhead; ++i)
                 if (tile + i < tile_end) {
-                    load(pages[i], t[i]);
+                    ge.template load<STREAM>(pages[i], t[i]);
                     fetch(pages[i], tile + kAhead + i);
                 }
         }
@@ -435,7 +406,7 @@ struct QuantisedColumns {
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 process(t[i], tile + i);
-                load(pages[i], t[i]);
+                ge.template load<STREAM>(pages[i], t[i]);
                 fetch(pages[i], tile + 2 * kAhead + i);
             }
         const int claimed = claim();  // the next item's counter is read under the last loads
@@ -444,172 +415,9 @@ struct QuantisedColumns {
             for (int i = 0; i < kAhead; ++i)
                 if (tile + i < tile_end) {
                     process(t[i], tile + i);
-                    if (tile + kAhead + i < tile_end) load(pages[i], t[i]);
+                    if (tile + kAhead + i < tile_end) ge.template load<STREAM>(pages[i], t[i]);
                 }
         return claimed;
-    }
-
-    // A step forms the scores of the next tile, the weights of this one and the output of the one before.  None waits for another, so they are
-    // laid out in groups of matrix instructions and the vector arithmetic that runs under them; the scheduling barriers keep the
-    // groups, which the compiler would gather.
-    __device__ __forceinline__ void over_cached(const AttnParams &p, const TileDesc &it, int kvh, int col0, int key_begin, int key_end, int lane) {
-        constexpr int kAhead = 2;
-        static_assert(kOperands == 2 * NC * PackedQueries<D>::kTerms, "as many score instructions as output operands");
-        const int g = lane >> 4;
-        init(p, it, kvh, col0, key_end, lane);
-
-        float top[NC];       // this lane's largest score
-        float raise_at[NC];  // the reference maximum is raised when one of them is larger
-        // Score instruction number SLOT of a tile: first of all pages and column groups, then the second ones that add to them.
-        auto score = [&](const QuantisedKeys &t, f32x4 (&to)[NC][2], auto slot) {
-            constexpr int SLOT = decltype(slot)::value, TERM = SLOT / (2 * NC), b = SLOT / NC % 2, cg = SLOT % NC;
-            const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-            to[cg][b] = packed[cg].template scores<TERM>(t.codes[b], t.scale[b], TERM == 0 ? zero : to[cg][b]);
-        };
-        auto mask_and_top = [&](QuantisedScales &t, int tile) {
-            mask(t.of, tile, g);
-#pragma unroll
-            for (int cg = 0; cg < NC; ++cg) top[cg] = largest_of(s[cg][0], s[cg][1]);
-        };
-        uint32_t pT[NC][4];  // the previous tile's weights, as bf16: the second operands of its output instructions
-#pragma unroll
-        for (int cg = 0; cg < NC; ++cg)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) pT[cg][i] = 0;
-        auto operand_of = [&](int cg) { return __builtin_bit_cast(bf16x8, u32x4{pT[cg][0], pT[cg][1], pT[cg][2], pT[cg][3]}); };
-        auto step = [&](const Values &before, const QuantisedScales &t, const QuantisedKeys &next, QuantisedScales &next_scales, int tile, auto load_more) {
-            bool higher = false;
-#pragma unroll
-            for (int cg = 0; cg < NC; ++cg) higher |= top[cg] > raise_at[cg];
-            if (__any(higher)) {
-#pragma unroll
-                for (int cg = 0; cg < NC; ++cg) {
-                    const float alpha = raise(cg, top[cg]);
-                    raise_at[cg] = (st[cg].m + kRescaleSlack) / scale;
-                    const u32x4 w = __builtin_bit_cast(u32x4, __builtin_convertvector(__builtin_convertvector(operand_of(cg), f32x8) * alpha, bf16x8));
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) pT[cg][i] = w[i];
-                }
-            }
-            f32x4 s_next[NC][2];
-            uint32_t p_new[NC][4];
-            float even = 0.f;
-            bf16x8 v = value_operand<0>(before);
-            bf16x8 p_old[NC];
-#pragma unroll
-            for (int cg = 0; cg < NC; ++cg) p_old[cg] = operand_of(cg);
-            auto weight = [&](int k) {
-                const int cg = k / 8, b = k / 4 % 2, i = k % 4;
-                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[cg][b][i], scale, -st[cg].m));
-                st[cg].l += e;
-                const float w = e * t.of[b][i];
-                // rounded to bf16 for the matrix instruction, as above
-                if (k & 1) {
-                    p_new[cg][k % 8 / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{even, w}, bf16x2));
-                    asm volatile("" : "+v"(p_new[cg][k % 8 / 2]), "+v"(st[cg].l));  // (they would be formed behind the next step's branch)
-                } else {
-                    even = w;
-                    asm volatile("" : "+v"(even), "+v"(st[cg].l));
-                }
-            };
-            __builtin_amdgcn_sched_barrier(0);
-            static_for<kOperands>([&](auto at) {
-                constexpr int c = decltype(at)::value;
-                score(next, s_next, at);
-#pragma unroll
-                for (int k = c * 8 * NC / kOperands; k < (c + 1) * 8 * NC / kOperands; ++k) weight(k);
-                __builtin_amdgcn_sched_barrier(0);
-                st[0].o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_old[0], st[0].o[c], 0, 0, 0);
-                bf16x8 v_next = v;
-                if constexpr (c + 1 < kOperands) v_next = value_operand<c + 1>(before);
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int cg = 1; cg < NC; ++cg) st[cg].o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_old[cg], st[cg].o[c], 0, 0, 0);
-                v = v_next;
-            });
-            load_more();
-#pragma unroll
-            for (int cg = 0; cg < NC; ++cg) {
-#pragma unroll
-                for (int b = 0; b < 2; ++b) s[cg][b] = s_next[cg][b];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) pT[cg][i] = p_new[cg][i];
-            }
-            mask_and_top(next_scales, tile + 1);
-        };
-
-        int tile = key_begin / kTileKeys;
-        const int tile_end = key_begin >= key_end ? tile : (key_end + kTileKeys - 1) / kTileKeys;
-        if (tile >= tile_end) return;
-        // Tile T lives in slot T - (first tile) modulo kAhead of three rings.  Its step takes the keys of T + 1, the values' scales of T and the values'
-        // codes of T - 1, and has those of kAhead tiles on loaded in their place; the table entries come a step before.  (Loads beyond the range:
-        // the sequence's last page again, at most.  The last step forms scores of whatever its neighbour's registers hold, which nothing reads.)
-        QuantisedKeys keys[kAhead];
-        QuantisedScales scales[kAhead];
-        Values values[kAhead];
-        QuantisedPages entries[kAhead + 2];
-#pragma unroll
-        for (int i = 0; i < kAhead + 2; ++i) entries[i] = ge.pages_of(tile + i);
-        QuantisedPages entry = ge.pages_of(tile + kAhead + 2);
-        QuantisedRecords for_values = ge.records(entries[kAhead - 1]), for_scales = ge.records(entries[kAhead]), for_keys = ge.records(entries[kAhead + 1]);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const QuantisedRecords r = ge.records(entries[i]);
-            ge.template load<false>(r, keys[i]);
-            ge.template load<false>(r, scales[i]);
-            if (i + 1 < kAhead) ge.template load<false>(r, values[i]);
-        }
-        static_for<kOperands>([&](auto slot) { score(keys[0], s, slot); });
-        ge.template load<false>(for_scales, keys[0]);
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int j = 0; j < D / 32; ++j) values[kAhead - 1].codes[b][j] = 0;  // (the tile before the first)
-#pragma unroll
-        for (int cg = 0; cg < NC; ++cg) raise_at[cg] = kNegSentinel;
-        mask_and_top(scales[0], tile);
-        for (; tile + 2 * kAhead < tile_end; tile += kAhead)
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                constexpr int k = kAhead;
-                const QuantisedRecords later = ge.records(entry);
-                entry = ge.pages_of(tile + i + kAhead + 3);
-                __builtin_amdgcn_sched_barrier(0);
-                step(values[(i + k - 1) % k], scales[i], keys[(i + 1) % k], scales[(i + 1) % k], tile + i, [&] {
-                    ge.renew();
-                    ge.template load<false>(for_keys, keys[(i + 1) % k]);
-                    ge.template load<false>(for_scales, scales[i]);
-                    ge.template load<false>(for_values, values[(i + k - 1) % k]);
-                });
-                for_values = for_scales;
-                for_scales = for_keys;
-                for_keys = later;
-            }
-        for (; tile < tile_end; tile += kAhead)
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i)
-                if (tile + i < tile_end) {
-                    constexpr int k = kAhead;
-                    const QuantisedRecords later = ge.records(entry);
-                    entry = ge.pages_of(tile + i + kAhead + 3);
-                    step(values[(i + k - 1) % k], scales[i], keys[(i + 1) % k], scales[(i + 1) % k], tile + i, [&] {
-                        ge.renew();
-                        if (tile + i + k + 1 < tile_end) ge.template load<false>(for_keys, keys[(i + 1) % k]);
-                        if (tile + i + k < tile_end) ge.template load<false>(for_scales, scales[i]);
-                        if (tile + i + k - 1 < tile_end) ge.template load<false>(for_values, values[(i + k - 1) % k]);
-                    });
-                    for_values = for_scales;
-                    for_scales = for_keys;
-                    for_keys = later;
-                    if (tile + i + 1 == tile_end)
-                        static_for<kOperands>([&](auto at) {
-                            constexpr int c = decltype(at)::value;
-                            const bf16x8 v = value_operand<c>(values[i]);
-#pragma unroll
-                            for (int cg = 0; cg < NC; ++cg) st[cg].o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, operand_of(cg), st[cg].o[c], 0, 0, 0);
-                        });
-                }
     }
 };
 
@@ -623,7 +431,7 @@ __device__ __forceinline__ int quantised_wave_path(const AttnParams &p, const Ti
     const int quarter = ((ur.key_end - ur.key_begin + 3) / 4 + kTileKeys - 1) / kTileKeys * kTileKeys;
     const int begin = min(ur.key_begin + wave * quarter, ur.key_end), end = min(begin + quarter, ur.key_end);
     QuantisedColumns<D, NC> columns;
-    const int claimed = columns.template over_streamed<STREAM>(p, it, kvh, 0, begin, end, tid & 63, [&] { return tid == 0 ? claim() : 0; });
+    const int claimed = columns.template run<STREAM, NC == 1 ? 4 : 2>(p, it, kvh, 0, begin, end, tid & 63, [&] { return tid == 0 ? claim() : 0; });
     wave_finish<D, QuantisedWaveSmem<D>>(p, it, split, kvh, tid, smem, columns.st[0]);
     if constexpr (NC == 2) {
         __syncthreads();
@@ -646,7 +454,7 @@ __device__ __forceinline__ void quantised_chunk_path(const AttnParams &p, const 
     const int prefix = it.ctx_len - it.q_len, first_row = (it.col_begin + col0) / p.group, last_row = (it.col_begin + min(col0 + 32, it.n_cols) - 1) / p.group;
     const int key_end = min(ur.key_end, prefix + last_row + 1);
     const int key_begin = p.window > 0 ? max(ur.key_begin, (prefix + first_row - p.window + 1) / kTileKeys * kTileKeys) : ur.key_begin;
-    columns.over_cached(p, it, kvh, col0, key_begin, key_end, lane);
+    columns.template run<false, 1>(p, it, kvh, col0, key_begin, key_end, lane, [] { return 0; });
 #pragma unroll
     for (int cg = 0; cg < 2; ++cg) {
         const SoftmaxState<D> &x = columns.st[cg];
