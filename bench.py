@@ -157,7 +157,7 @@ def run_serving(args) -> int:
     def run(reqs, policy, budget=512, linear_model=None):
         pages = int(1.3 * sum((r.total_rows + 15) // 16 for r in reqs))
         loop = serving.ServingLoop(wl.MISTRAL_7B, reqs, serving.GpuBackend(seed=seed, keep_outputs=False, options=opts,
-                                                                             linear_model=linear_model),
+                                                                             linear_model=linear_model, cache=args.cache),
                                    num_pages=pages, token_budget=budget, chunk_size=budget, max_batch_size=128, policy=policy,
                                    seed=seed)
         return loop.run()
@@ -179,7 +179,7 @@ def run_serving(args) -> int:
         "vs_baseline": None, "dtype": "bf16", "data": "synthetic",
         "config": {"workload": "serve: %d requests, Poisson 8000/s, prompts lognormal(median 1730, p90 5696) <= 8192, outputs "
                                "lognormal(median 415, p90 834) <= 256, Mistral-7B attention shape, token budget 512" % n_req,
-                   "attention_rows": tokens, "seed": seed},
+                   "attention_rows": tokens, "seed": seed, **({"cache": args.cache} if args.cache != "bf16" else {})},
         "policies": out,
         "policies_with_linear_layers": out_l}))
     return 0
@@ -192,7 +192,8 @@ def run_token_budget(args) -> int:
     seed = 41 if args.seed is None else args.seed
     rng = np.random.default_rng([seed, 0x7B])
     decode_ctx = rng.integers(256, 4096 + 1, size=64).tolist()
-    timer = tb.gpu_timer({k: int(v) for k, v in (kv.split("=") for kv in args.opt)}, reps=max(5, min(args.steps, 30)))
+    timer = tb.gpu_timer({k: int(v) for k, v in (kv.split("=") for kv in args.opt)}, reps=max(5, min(args.steps, 30)),
+                         cache=args.cache)
     rows = tb.profile(timer, wl.MISTRAL_7B, [64, 128, 256, 512, 1024, 2048, 4096], decode_ctx, chunk_prefix=2048, seed=seed)
     targets = [150e-6, 200e-6, 300e-6, 500e-6]
     picks = {"%d us" % round(t * 1e6): tb.compute_token_budget(rows, t) for t in targets}
@@ -201,7 +202,7 @@ def run_token_budget(args) -> int:
     # the same with the four linear layers of one Mistral-7B transformer layer in the iteration (section 3.1: the
     # operators that dominate it); tile quantisation now shows at the linear layers' 128/256-token tiles
     timer_l = tb.gpu_timer({k: int(v) for k, v in (kv.split("=") for kv in args.opt)}, reps=max(5, min(args.steps, 30)),
-                           linear_model="mistral-7b")
+                           linear_model="mistral-7b", cache=args.cache)
     rows_l = tb.profile(timer_l, wl.MISTRAL_7B, [64, 128, 256, 512, 1024, 2048, 4096], decode_ctx, chunk_prefix=2048, seed=seed)
     targets_l = [300e-6, 500e-6, 1000e-6, 2000e-6]
     picks_l = {"%d us" % round(t * 1e6): tb.compute_token_budget(rows_l, t) for t in targets_l}
@@ -212,7 +213,7 @@ def run_token_budget(args) -> int:
         "ms_per_step": t512 * 1e3, "higher_is_better": True, "scaling": "weak", "vs_baseline": None, "dtype": "bf16",
         "data": "synthetic",
         "config": {"workload": "budget: Mistral-7B attention shape, 64 decodes ctx U[256,4096] + one chunk of (budget - 64) tokens "
-                               "@prefix 2048", "seed": seed},
+                               "@prefix 2048", "seed": seed, **({"cache": args.cache} if args.cache != "bf16" else {})},
         "profile_us": {str(r["token_budget"]): r["seconds"] * 1e6 for r in rows},
         "largest_budget_within": picks,
         "tile_quantization_us": {str(r["chunk"]): r["seconds"] * 1e6 for r in quant},
@@ -355,6 +356,8 @@ def main() -> int:
                     help="normal: the workloads' N(0,1) values (every reported figure); zeros: all-zero Q/K/V or x/w, a "
                          "diagnostic that shows how far the chip's clock, which falls with the matrix pipes' switching "
                          "power, moves the MFMA-bound kernels (no parity check, no CPU baseline)")
+    ap.add_argument("--cache", choices=["bf16", "4bit"], default="bf16",
+                    help="serve and budget only: the key/value cache, bf16 or in 4 bits (0.27 of the bytes)")
     ap.add_argument("--sweep-chunks", default="", help="c5_sweep only: comma-separated chunk sizes (default: 8192,2048,...,64)")
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--no-kernel-timing", action="store_true")
@@ -376,6 +379,9 @@ def main() -> int:
 
     if args.values == "zeros" and args.workload in ("c5_sweep", "serve", "budget", "decode_probe"):
         sys.stderr.write("bench.py: --values zeros applies to the single-batch workloads and to --workload linear\n")
+        return 2
+    if args.cache != "bf16" and args.workload not in ("serve", "budget"):
+        sys.stderr.write("bench.py: --cache applies to --workload serve and budget\n")
         return 2
     if args.workload == "c5_sweep":
         return run_sweep(args, binding, harness, torch)

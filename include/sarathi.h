@@ -236,6 +236,7 @@ sarathi_status sarathi_hybrid_attention_noalloc(sarathi_handle *handle,
  * max |v| <= 6 * m * 2^e, not below 2^-100, not above 2^124.  A block of keys that holds an infinity or NaN has the byte 255 and stands for
  * NaN; values that hold one have the scale NaN.  What a record stands for is exact in bf16.  Hidden positions (beyond ctx_len, behind
  * a row's own, in front of its window) influence no result, whatever their slots hold, NaN and infinities included.
+ * Attention takes a query as it is where a channel is more than 2^-15 of its head's largest one, and to 2^-23 of that elsewhere.
  *
  * sarathi_quantised_page_bytes: bytes of a page, all KV heads.  kv_cache, k_new, v_new, k_rows and v_rows are 16-byte aligned, else
  * SARATHI_EINVAL.  Everything else is as for the functions of the same name without _quantised: a handle serves both kinds of
