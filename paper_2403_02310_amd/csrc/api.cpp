@@ -224,8 +224,8 @@ Schedule schedule_of(const sarathi_handle *h) {
         // keys (41 decodes, 1000 blocks: 115.1 us with one, 110.6 with two; 15 decodes 20.5 and 18.9) and 1.38 x (30.0
         // and 30.8; at 1.7 to 1.8 x, where short decodes stay whole next to the pieces, 31.1 and 34.1, 53.6 and 69.6).
         // Over the 4-bit cache a block has four times the keys to go through for its bytes, and two on a unit run under each other's waits (us a
-        // call, one and two: 200 decodes, 58 and 2 heads of 64, 50.8 and 44.5; 81, 32 and 8 heads, 42.3 and 37.2; 53, 64 and 8, 20.6
-        // and 19.0; but 42, 56 and 8, 33.2 and 34.5).
+        // call, one and two: 200 decodes, 58 and 2 heads of 64, 53.4 and 43.3; 81, 32 and 8 heads, 40.9 and 37.6; 53, 64 and 8, 20.3
+        // and 18.7; but 42, 56 and 8, 31.5 and 34.2).
         const bool quantised = pl.key_bytes != h->cfg.head_dim * 4.0;
         const bool one = h->opt.decode_blocks_per_cu == 1 ||
                          (h->opt.decode_blocks_per_cu < 0 && wave_blocks <= 1024 && !pl.even_decode_pieces && !quantised);

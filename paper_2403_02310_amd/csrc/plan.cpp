@@ -460,8 +460,8 @@ WaveCut cheapest_wave_cut(const sarathi_config &cfg, const Plan &plan, size_t n_
     const double key_us = plan.key_bytes;  // of a key and its value, one KV head
     // Over the 4-bit cache a block alone pulls 40 GB/s as well (320 keys a microsecond; with 64 channels 26 and 370), of fewer bytes, and the merge
     // is cheap against it, so that cuts pay from 9 us by the estimate on (us a call, whole and cut: two decodes of up to 4725 keys, 16 and 2 heads,
-    // 21.8 and 12.0; 10 of up to 2270, 32 and 8 heads, 14.9 and 12.3; 3 of up to 1779, 56 and 8 heads, 13.0 and 11.0; 12 of up to 1202 11.6 and
-    // 12.8; 11 of up to 1541, 58 and 2 heads of 64 channels, 13.5 and 11.6).
+    // 20.0 and 12.6; 10 of up to 2270, 32 and 8 heads, 14.3 and 12.9; 3 of up to 1779, 56 and 8 heads, 12.5 and 12.0; 12 of up to 1202 11.7 and
+    // 13.0; 11 of up to 1541, 58 and 2 heads of 64 channels, 13.4 and 12.7).
     const bool quantised = plan.key_bytes != cfg.head_dim * 4.0;
     const double block_rate = quantised && cfg.head_dim == 64 ? 26.0e3 : 40.0e3, merge_us = quantised ? 2.5 : 5.3;
     double chunk_steps = 0.0;
@@ -585,11 +585,12 @@ bool chunks_as_wave_tiles(const sarathi_config &cfg, const Options &opt, const W
 
 // The same over the 4-bit cache, whose wave tiles of 32 columns reach 0.93 of the chunk tiles' rate where both fill the chip and come in four
 // times as many blocks.  They pay as long as those are few, and where the keys are not: a block's start and its four wavefronts' merge
-// want some work between them.  Next to decodes that stream for more than 0.3 of the time a chunk block takes, chunk tiles pay, which leave
-// them a slot on every compute unit, unless those are few and wait for a block longer than the chunk takes.  us a call, chunk tiles and wave tiles: 235 tokens behind 1258, 64 and 8 heads, 35.3 and 26.6; 580 behind 1774,
-// 58 and 2 heads of 64 channels, next to 6 decodes 50.4 and 39.4; 488 behind 3165 next to 186 of up to 777, 64 and 8 heads, 90.5 and 81.3; but
-// 272 behind 1 16.3 and 18.4, 1299 behind none and 749 behind 4211 145 and 156; 512 behind 1871 next to 64 of up to 4096, 32 and 8 heads, 56 and 71,
-// and 8 behind 410 next to 29 of up to 7659, 16 and 2 heads, 20.0 and 16.4.
+// want some work between them.  Next to decodes that stream for more than 0.75 of the time a chunk block takes, chunk tiles leave those
+// a slot on every compute unit, which pays unless the decodes are few and wait for a block longer than the chunk takes.  us a call, chunk tiles and
+// wave tiles: 235 tokens behind 1258, 64 and 8 heads, 34.9 and 22.6; 580 behind 1774, 58 and 2 heads of 64 channels, next to 6 decodes 51.1 and 38.6;
+// 532 behind 1801 next to 119 of up to 1150, 32 and 8 heads, 53.6 and 39.8; but 272 behind 1, 64 and 8 heads, 15.1 and 16.7, 1299 behind none and 749
+// behind 4211 143 and 153; 400 behind 2072 next to 157 of up to 4383, 56 and 8 heads, 88 and 97.  Of 46 drawn batches below the line the average is 0.86 x,
+// the worst 1.035 x, of 24 above it 0.95 x and 1.10 x.
 bool quantised_chunks_as_wave_tiles(const sarathi_config &cfg, const Options &opt, const WorkspaceLayout &ws, const int32_t *q_len,
                                     const int32_t *ctx_len, int32_t num_seqs) {
     if (opt.tile_split_keys > 0 || opt.resident_chunks == 1 || opt.interleave != 2) return false;  // asks for chunk tiles
@@ -612,7 +613,7 @@ bool quantised_chunks_as_wave_tiles(const sarathi_config &cfg, const Options &op
     const double key_bytes = (double)quantised_record_bytes(cfg.head_dim) / kPageSize;
     const double stream_us = (double)other_keys * cfg.num_kv_heads * key_bytes / 6.5e6;
     const double other_us = (double)other_span * key_bytes / (cfg.head_dim == 128 ? 40.0e3 : 26.0e3);
-    if (stream_us > 0.3 * chunk_us && other_us < std::max(chunk_us, stream_us)) return false;
+    if (stream_us > 0.75 * chunk_us && other_us < std::max(chunk_us, stream_us)) return false;
     // a plan that travels in kernel arguments has to fit one launch so
     return ws.meta_per_launch == 0 || attn_meta_bytes((size_t)tiles, (size_t)tiles, 0) <= ws.meta_per_launch;
 }
