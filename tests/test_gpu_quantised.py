@@ -433,3 +433,32 @@ def test_randomized_batches_shapes_and_options(hx):
         max_ctx = int(rng.choice([60, 400, 1500, 4000]))
         b = wl.random_hybrid(9000 + case, shape, n_chunks, n_dec, max_chunk=min(int(rng.choice([8, 130, 400])), max_ctx), max_ctx=max_ctx)
         _check(hx, b, opts, what="case %d %s" % (case, shape))
+
+
+@pytest.mark.parametrize("shape", ["gqa4_d128", "gqa29_d64"])
+def test_queries_with_an_outlying_channel(hx, shape):
+    """A query channel 2^13 times the others, against keys that are zero there: the other channels decide.  A query number is off by at most
+    2^-23 of its head's largest, 2^-10 here; over the channels, whose signs are random, a score is off by about 2^-10 of a key's norm
+    over sqrt(D), a thousandth, and a weight by as much of itself: a quarter of its rounding to bf16."""
+    s = SHAPES[shape]
+    q_len, ctx = [1, 64, 1], [700, 333, 65]
+    b = wl._make("outlier", s, q_len, ctx, 48)
+    h = hx.make_handle(b)
+    pool = hx.make_quantised_pool(h, b.num_pages, 0xFF)
+    bt = torch.from_numpy(b.block_table).cuda()
+    zero, ks, vs = np.zeros(1, np.int32), [], []
+    for i in range(b.num_seqs):
+        k, v = (x.copy() for x in b.kv_bits(i))
+        k[..., 5] = 0
+        n = np.array([ctx[i]], np.int32)
+        h.kv_append_quantised(hx.bits_to_device(k), hx.bits_to_device(v), pool, bt[i:i + 1], zero, n, n)
+        held = qref.stands_for(k, v)
+        ks.append(held[0]), vs.append(held[1])
+    q_bits = b.q_bits(0).copy()
+    q_bits[..., 5] = wl.f32_to_bf16_bits(np.float32([8192.0]))[0]
+    q = hx.bits_to_device(q_bits)
+    out = torch.empty_like(q)
+    h.hybrid_attention_quantised(q, pool, bt, b.q_start, b.q_len, b.ctx_len, b.sm_scale, out)
+    v = np.concatenate(vs)
+    ref = oracle.hybrid_attention(q_bits, np.concatenate(ks), v, b.kv_start, b.q_start, b.q_len, b.ctx_len, b.sm_scale)
+    compare(hx.bf16_tensor_to_f64(out), ref, b.name, np.abs(qref._f64(v)).max())
